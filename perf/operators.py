@@ -31,29 +31,29 @@ def _cross(name, op, seqs, q, kv, hq, hkv, d, dtype="bf16", empty=0, padded=Fals
 def listed():
     return [
         # one new token of each running request, far into a context that was stretched four times: latency
-        _rope("rope, one token each", 16, 1, 1, 30000, 32, 8, 128, 128, "half", "parts", "bf16", magnitude=1.1),
+        _rope("rope one token each", 16, 1, 1, 30000, 32, 8, 128, 128, "half", "parts", "bf16", magnitude=1.1),
         # a packed training batch straight out of the fused projection, Q and K together
-        _rope("rope, packed batch", 12, 64, 8192, 0, 32, 8, 128, 128, "half", "parts", "bf16", fused=True, shape=2),
+        _rope("rope packed batch", 12, 64, 8192, 0, 32, 8, 128, 128, "half", "parts", "bf16", fused=True, shape=2),
         # the gradients of Q and K of a model that turns neighbouring pairs of the first half of each head
-        _rope("rope, gradients, interleaved", 9, 100, 6000, 0, 40, 40, 128, 64, "interleaved", "plain", "bf16", inverse=True, shape=3),
+        _rope("rope gradients interleaved", 9, 100, 6000, 0, 40, 40, 128, 64, "interleaved", "plain", "bf16", inverse=True, shape=3),
         # a numerical check in fp32, a head and a turned part that are no power of two
-        _rope("rope, fp32, odd heads", 37, 1, 400, 0, 7, 1, 80, 24, "half", "linear", "fp32", shape=4),
+        _rope("rope fp32 odd heads", 37, 1, 400, 0, 7, 1, 80, 24, "half", "linear", "fp32", shape=4),
         # transcription: one token each against a few seconds to half a minute of sound, the smallest attention call
-        _cross("cross, one token each", "cross_fwd", 4, (1, 1), (1500, 1500), 20, 20, 64),
+        _cross("cross one token each", "cross_fwd", 4, (1, 1), (1500, 1500), 20, 20, 64),
         # serving: one token of each of 64 requests against long documents in a padded cache
-        _cross("cross, padded cache", "cross_fwd", 64, (1, 1), (500, 8192), 32, 8, 128, padded=True, shape=5),
+        _cross("cross padded cache", "cross_fwd", 64, (1, 1), (500, 8192), 32, 8, 128, padded=True, shape=5),
         # a training batch of speech and transcripts, two clips without sound
-        _cross("cross, ragged batch", "cross_fwd", 24, (1, 448), (1, 1500), 20, 20, 64, empty=2, shape=6),
+        _cross("cross ragged batch", "cross_fwd", 24, (1, 448), (1, 1500), 20, 20, 64, empty=2, shape=6),
         # long documents and long answers
-        _cross("cross, long", "cross_fwd", 6, (1500, 6000), (4000, 12000), 32, 8, 128, shape=7),
+        _cross("cross long", "cross_fwd", 6, (1500, 6000), (4000, 12000), 32, 8, 128, shape=7),
         # gradients of the training batch
-        _cross("cross gradients, ragged", "cross_bwd", 24, (1, 448), (1, 1500), 20, 20, 64, empty=2, shape=6),
+        _cross("cross gradients ragged", "cross_bwd", 24, (1, 448), (1, 1500), 20, 20, 64, empty=2, shape=6),
         # gradients of an image model that looks at a prompt: many rows, few keys
-        _cross("cross gradients, few keys", "cross_bwd", 16, (1024, 4096), (8, 77), 8, 8, 64, shape=8),
+        _cross("cross gradients few keys", "cross_bwd", 16, (1024, 4096), (8, 77), 8, 8, 64, shape=8),
         # gradients of long documents and long answers
-        _cross("cross gradients, long", "cross_bwd", 4, (1500, 6000), (4000, 12000), 32, 8, 128, shape=9),
+        _cross("cross gradients long", "cross_bwd", 4, (1500, 6000), (4000, 12000), 32, 8, 128, shape=9),
         # gradients of a numerical check in fp32
-        _cross("cross gradients, fp32", "cross_bwd", 7, (1, 500), (1, 900), 8, 2, 128, dtype="fp32", empty=1, shape=10),
+        _cross("cross gradients fp32", "cross_bwd", 7, (1, 500), (1, 900), 8, 2, 128, dtype="fp32", empty=1, shape=10),
     ]
 
 
