@@ -320,6 +320,51 @@ hyd_status hyd_rope_packed(const void* x, const int32_t* cu_seqlens, int num_seq
                            void* out, void* hip_stream);
 
 /*
+ * Rotary positions in general form, for models whose heads, layouts or contexts hyd_rope_packed does not cover, and for
+ * serving.  Pair p of a head, p in [0, rot_dim / 2), is (x[p], x[p + rot_dim / 2]) with HYD_ROPE_HALF and (x[2 p], x[2 p + 1])
+ * with HYD_ROPE_INTERLEAVED.  At position m it becomes
+ *     magnitude * (a cos - b sin),  magnitude * (b cos + a sin),   angle = m * freqs[p];
+ * the head's other head_dim - rot_dim elements are copied.  inverse != 0 negates the angle: the transpose of the map
+ * (magnitude included), which carries gradients back.
+ *
+ *   q, q_out         device, total_tokens rows of hq heads, the heads of a row contiguous, rows q_stride / q_out_stride
+ *                    elements apart (>= hq * head_dim), so that q may be a part of a fused projection.  q_out may be q, with
+ *                    the same stride; otherwise they do not overlap.
+ *   k, k_out         a second tensor for the same rows and positions, e.g. K; hkv = 0: none.  hq and hkv are free of each other.
+ *   positions        device int32[total_tokens], the position of every row, or NULL; then
+ *   cu_seqlens       device int32[num_seqs+1], non-decreasing, cu[0] >= 0: row t of sequence s has position
+ *   starts           t - cu[s] + starts[s] (device int32[num_seqs], e.g. the tokens a request holds already; NULL: 0).  Rows in front
+ *                    of cu[0] and from cu[num_seqs] on are left as they were.
+ *   freqs            device double[rot_dim / 2] (hyd_rope_frequencies makes them)
+ *   head_dim         2..1024; rot_dim even, 2..head_dim.  (hq + hkv) * head_dim up to 2^20.
+ * HYD_BF16 and HYD_FP32; the angle is reduced in double, one rounding of the result.  No workspace; one kernel, bound by HBM.
+ * It moves 16 bytes at a time where head_dim, rot_dim / 2, strides and addresses are multiples of that, else less.
+ * Errors: HYD_ERR_SHAPE (sizes, strides, layout, addresses that are no multiple of an element), HYD_ERR_HEADS, HYD_ERR_HEADDIM,
+ * HYD_ERR_DTYPE, HYD_ERR_NULL.
+ */
+typedef enum { HYD_ROPE_HALF = 0, HYD_ROPE_INTERLEAVED = 1 } hyd_rope_layout;
+typedef enum { HYD_ROPE_PLAIN = 0, HYD_ROPE_LINEAR = 1, HYD_ROPE_PARTS = 2 } hyd_rope_scaling;
+
+hyd_status hyd_rope_rotate(const void* q, int hq, int64_t q_stride, void* q_out, int64_t q_out_stride,
+                           const void* k, int hkv, int64_t k_stride, void* k_out, int64_t k_out_stride,
+                           const int32_t* cu_seqlens, const int32_t* starts, int num_seqs, const int32_t* positions,
+                           int total_tokens, int head_dim, const double* freqs, int rot_dim, hyd_rope_layout layout,
+                           float magnitude, int inverse, hyd_dtype dt, void* hip_stream);
+
+/*
+ * Frequencies f_p = base^(-2 p / rot_dim) of the pairs, into HOST memory (rot_dim / 2 doubles), scaled for contexts longer
+ * than a model was trained on:
+ *   HYD_ROPE_PLAIN    as they are (factor, original_length, low, high are not looked at)
+ *   HYD_ROPE_LINEAR   f_p / factor: positions are interpolated
+ *   HYD_ROPE_PARTS    by parts: a pair that turns r = original_length * f_p / (2 pi) times within the original context keeps its
+ *                     frequency if r >= high, is interpolated if r <= low, and lies linearly (in r) between the two otherwise
+ * HYD_ERR_HEADDIM: rot_dim odd or outside 2..1024; HYD_ERR_SHAPE: base <= 1, factor <= 0, original_length <= 0, low < 0, high <= low,
+ * or not finite.  No HIP call.
+ */
+hyd_status hyd_rope_frequencies(int rot_dim, double base, hyd_rope_scaling scaling, double factor, double original_length,
+                                double low, double high, double* freqs);
+
+/*
  * Timing hook for benchmarks.  While enabled (on != 0), every kernel that a later call of this
  * library enqueues from this host thread is bracketed with HIP events on the caller's stream and
  * appended to a per-thread list (at most 8192 launches; further ones are not recorded).  Nothing

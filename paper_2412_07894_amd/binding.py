@@ -19,9 +19,11 @@ EXPORTS = (
     "hyd_varlen_attn_fwd_range", "hyd_varlen_attn_bwd_range", "hyd_attn_merge", "hyd_rope_packed",
     "hyd_varlen_attn_fwd_noalloc", "hyd_varlen_attn_fwd_noalloc_max_workspace",
     "hyd_varlen_attn_schedule_status", "hyd_varlen_attn_schedule_layout",
-    "hyd_varlen_attn_fwd_rope", "hyd_varlen_attn_bwd_rope",
+    "hyd_varlen_attn_fwd_rope", "hyd_varlen_attn_bwd_rope", "hyd_rope_rotate", "hyd_rope_frequencies",
 )
 RANGE_ALIGN = 256   # HYD_RANGE_ALIGN of the header
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}                  # hyd_rope_layout
+ROPE_SCALINGS = {"plain": 0, "linear": 1, "parts": 2}         # hyd_rope_scaling
 
 
 class HydError(RuntimeError):
@@ -73,6 +75,11 @@ def load():
     lib.hyd_attn_merge.argtypes = [vp, vp, vp, vp, i, i, i, i, vp, vp, vp]
     lib.hyd_rope_packed.restype = i
     lib.hyd_rope_packed.argtypes = [vp, ip, i, i, i, i, f, i, i, vp, vp]
+    l, dbl = ctypes.c_int64, ctypes.c_double
+    lib.hyd_rope_rotate.restype = i
+    lib.hyd_rope_rotate.argtypes = [vp, i, l, vp, l, vp, i, l, vp, l, ip, ip, i, ip, i, i, vp, i, i, f, i, i, vp]
+    lib.hyd_rope_frequencies.restype = i
+    lib.hyd_rope_frequencies.argtypes = [i, dbl, i, dbl, dbl, dbl, dbl, vp]
     lib.hyd_enable_kernel_timing.restype = None
     lib.hyd_enable_kernel_timing.argtypes = [i]
     lib.hyd_kernel_times.restype = i
@@ -119,6 +126,26 @@ def _host_ptr(cu_host):
 def _stream_ptr(stream):
     s = torch.cuda.current_stream() if stream is None else stream
     return ctypes.c_void_p(s.cuda_stream)
+
+
+class _on:
+    """The device of a call's tensors, made the current one where it is not."""
+    def __init__(self, device):
+        if device.type != "cuda":
+            raise ValueError(f"tensors must be on a GPU, got {device}")
+        self.other = torch.cuda.device(device) if device.index != torch.cuda.current_device() else None
+
+    def __enter__(self):
+        if self.other is not None:
+            self.other.__enter__()
+
+    def __exit__(self, *exc):
+        if self.other is not None:
+            self.other.__exit__(*exc)
+
+
+def _stream_of(device, stream):
+    return (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream
 
 
 def varlen_attn_fwd(q, k, v, cu_seqlens, max_seqlen, softmax_scale, cu_seqlens_host=None,
@@ -276,6 +303,78 @@ def rope_packed(x, cu_seqlens, base=10000.0, inverse=False, out=None, stream=Non
     _check(load().hyd_rope_packed(x.data_ptr(), cu_seqlens.data_ptr(), cu_seqlens.numel() - 1, T, h, d, float(base),
                                   int(bool(inverse)), _dtype_code(x), out.data_ptr(), _stream_ptr(stream)))
     return out
+
+
+def rope_frequencies(rot_dim, base=10000.0, scaling="plain", factor=1.0, original_length=0.0, low=1.0, high=32.0, device="cuda"):
+    """Frequencies of the rot_dim / 2 pairs for rope_rotate, as a float64 tensor on `device`: made once per model.  `scaling`:
+    "plain", "linear" or "parts" (see hyd_rope_frequencies)."""
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError(f"scaling must be one of {sorted(ROPE_SCALINGS)}, got {scaling!r}")
+    out = np.zeros(max(int(rot_dim) // 2, 1), dtype=np.float64)
+    _check(load().hyd_rope_frequencies(int(rot_dim), float(base), ROPE_SCALINGS[scaling], float(factor), float(original_length),
+                                       float(low), float(high), out.ctypes.data))
+    return torch.from_numpy(out).to(device)
+
+
+def _rope_tensor(name, x, out, T, d, dt, device):
+    """Checks a tensor of rope_rotate and its output (made if None): [T, heads, d], the heads of a token contiguous."""
+    if x.dim() != 3 or x.shape[0] != T or x.shape[2] != d or x.dtype != dt or x.device != device:
+        raise ValueError(f"{name} must be [{T}, heads, {d}] in {dt} on {device}, got {tuple(x.shape)} {x.dtype} {x.device}")
+    if out is None:
+        out = torch.empty(x.shape, dtype=dt, device=device)
+    if out.shape != x.shape or out.dtype != dt or out.device != device:
+        raise ValueError(f"the output of {name} must be like it, got {tuple(out.shape)} {out.dtype} {out.device}")
+    row = x.shape[1] * d
+    strides = []
+    for t in (x, out):
+        if T and ((d > 1 and t.stride(2) != 1) or (t.shape[1] > 1 and t.stride(1) != d) or (T > 1 and t.stride(0) < row)):
+            raise ValueError(f"{name}: the heads of a token must be contiguous, got strides {t.stride()}")
+        strides.append(t.stride(0) if T > 1 else row)
+    return out, strides[0], strides[1]
+
+
+def _int32(name, t, n, device):
+    """A device int32 tensor of n elements (or None) as a pointer."""
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or not t.is_contiguous() or t.numel() != n or t.device != device:
+        raise ValueError(f"{name} must be a contiguous int32 tensor of {n} elements on {device}, got {t.dtype} {tuple(t.shape)} {t.device}")
+    return t.data_ptr()
+
+
+def rope_rotate(q, freqs, k=None, cu_seqlens=None, starts=None, positions=None, layout="half", magnitude=1.0, inverse=False,
+                out=None, k_out=None, stream=None):
+    """Rotary positions on q[T,H,d] and, with k[T,Hk,d], on both in one launch (bf16 or fp32, the rows may be strided); the first
+    2 * freqs.numel() elements of every head are turned.  The rows' positions are `positions` (int32 [T]) or follow from
+    cu_seqlens (int32 [num_seqs+1]) and `starts` (int32 [num_seqs] or None).  out may be q, k_out may be k.  Returns out, or
+    (out, k_out).  Work goes to `stream`, by default the current one of q's device."""
+    if q.dim() != 3:
+        raise ValueError(f"q must be [T, heads, d], got {tuple(q.shape)}")
+    T, hq, d = q.shape
+    dt, dev = _dtype_code(q), q.device
+    if layout not in ROPE_LAYOUTS:
+        raise ValueError(f"layout must be one of {sorted(ROPE_LAYOUTS)}, got {layout!r}")
+    if freqs.dtype != torch.float64 or not freqs.is_contiguous() or freqs.device != dev:
+        raise ValueError(f"freqs must be a contiguous float64 tensor on {dev}, got {freqs.dtype} {freqs.device}")
+    if (cu_seqlens is None) == (positions is None):
+        raise ValueError("either cu_seqlens or positions")
+    if starts is not None and cu_seqlens is None:
+        raise ValueError("starts go with cu_seqlens")
+    nseq = 0 if cu_seqlens is None else cu_seqlens.numel() - 1
+    if nseq < 0:
+        raise ValueError("cu_seqlens must have num_seqs + 1 elements")
+    out, qs, qos = _rope_tensor("q", q, out, T, d, q.dtype, dev)
+    hk, ks, kos = 0, 0, 0
+    if k is not None:
+        k_out, ks, kos = _rope_tensor("k", k, k_out, T, d, q.dtype, dev)
+        hk = k.shape[1]
+    with _on(dev):
+        _check(load().hyd_rope_rotate(q.data_ptr(), hq, qs, out.data_ptr(), qos, k.data_ptr() if hk else None, hk, ks,
+                                      k_out.data_ptr() if hk else None, kos, _int32("cu_seqlens", cu_seqlens, nseq + 1, dev),
+                                      _int32("starts", starts, nseq, dev), nseq, _int32("positions", positions, T, dev), T, d,
+                                      freqs.data_ptr(), 2 * freqs.numel(), ROPE_LAYOUTS[layout], float(magnitude),
+                                      int(bool(inverse)), dt, _stream_of(dev, stream)))
+    return out if k is None else (out, k_out)
 
 
 def enable_kernel_timing(on):

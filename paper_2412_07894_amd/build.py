@@ -2,11 +2,13 @@
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhyd_attn.so")
-SOURCES = [os.path.join(CSRC, "hyd_api.hip"), os.path.join(CSRC, "hyd_plan.cpp")]
+SOURCES = [os.path.join(CSRC, f) for f in ("hyd_api.hip", "hyd_rotary.hip", "hyd_plan.cpp")]
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -24,8 +26,7 @@ def sources_newer_than_lib():
     return any(os.path.getmtime(f) > t for f in deps)
 
 
-def build(verbose=False, extra_flags=()):
-    cmd = ["hipcc", *HIPCC_FLAGS, *extra_flags, *SOURCES, "-o", LIB]
+def _run(cmd, verbose):
     if verbose:
         print(" ".join(cmd), flush=True)
     r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
@@ -35,6 +36,15 @@ def build(verbose=False, extra_flags=()):
         raise RuntimeError("hipcc failed:\n" + out)
     if verbose and out.strip():
         print(out)
+
+
+def build(verbose=False, extra_flags=()):
+    """Compiles the sources next to each other and links them in their order."""
+    with tempfile.TemporaryDirectory() as tmp, ThreadPoolExecutor(len(SOURCES)) as pool:
+        objects = [os.path.join(tmp, os.path.basename(s) + ".o") for s in SOURCES]
+        flags = [f for f in HIPCC_FLAGS if f != "-shared"]
+        list(pool.map(lambda so: _run(["hipcc", *flags, *extra_flags, "-c", so[0], "-o", so[1]], verbose), zip(SOURCES, objects)))
+        _run(["hipcc", "--offload-arch=gfx950", "-shared", *objects, "-o", LIB], verbose)
     return LIB
 
 

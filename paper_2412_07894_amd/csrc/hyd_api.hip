@@ -14,6 +14,7 @@
 #include "hyd_fp32.h"
 #include "hyd_fwd_bf16.h"
 #include "hyd_fwd_coop.h"
+#include "hyd_host.h"
 #include "hyd_merge.h"
 #include "hyd_rope.h"
 
@@ -433,7 +434,6 @@ hyd_status device_info(DeviceInfo** out) {
 }
 
 // ---- benchmark hooks --------------------------------------------------------------------------
-struct TimedKernel { const char* name; hipEvent_t e0, e1; };
 thread_local bool t_timing = false;
 thread_local std::vector<TimedKernel> t_timed;
 thread_local WgTrace t_trace = {nullptr, 0};
@@ -445,19 +445,33 @@ void timed_clear() {
 
 constexpr size_t kMaxTimed = 8192;      // launches recorded between two reads of the list
 
-struct KernelTimer {       // brackets one launch with events when timing is on
-    hipStream_t st; bool on; TimedKernel tk;
-    KernelTimer(const char* name, hipStream_t s) : st(s), on(t_timing && t_timed.size() < kMaxTimed) {
-        tk.name = name;
-        if (on) {
-            on = hipEventCreate(&tk.e0) == hipSuccess && hipEventCreate(&tk.e1) == hipSuccess;
-            if (on) (void)hipEventRecord(tk.e0, st);
-        }
+}  // namespace
+
+namespace hyd {
+
+KernelTimer::KernelTimer(const char* name, hipStream_t s) : st(s), on(t_timing && t_timed.size() < kMaxTimed) {
+    tk.name = name;
+    if (on) {
+        on = hipEventCreate(&tk.e0) == hipSuccess && hipEventCreate(&tk.e1) == hipSuccess;
+        if (on) (void)hipEventRecord(tk.e0, st);
     }
-    ~KernelTimer() {
-        if (on) { (void)hipEventRecord(tk.e1, st); t_timed.push_back(tk); }
-    }
-};
+}
+KernelTimer::~KernelTimer() {
+    if (on) { (void)hipEventRecord(tk.e1, st); t_timed.push_back(tk); }
+}
+
+hyd_status current_device(int* device, int* cus) {
+    DeviceInfo* d = nullptr;
+    const hyd_status st = device_info(&d);
+    if (st != HYD_OK) return st;
+    *device = (int)(d - g_dev);
+    *cus = d->cus;
+    return HYD_OK;
+}
+
+}  // namespace hyd
+
+namespace {
 
 // View of a schedule of `tile` rows (a 2^split-th of the kernel's tile); its level count is bounded by the caller's max_seqlen.
 // `heads` work items per record are shared by `wgs` workgroups.  Sequences are grouped up to
