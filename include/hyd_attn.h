@@ -320,6 +320,40 @@ hyd_status hyd_rope_packed(const void* x, const int32_t* cu_seqlens, int num_seq
                            void* out, void* hip_stream);
 
 /*
+ * Cross attention of packed batches: the queries of sequence s, rows [cu_q[s], cu_q[s+1]) of one buffer, see every valid key of
+ * sequence s, rows [cu_kv[s], cu_kv[s] + n_s) of another one, e.g. an encoder's states.  The lengths have nothing to do with
+ * each other; n_s = cu_kv[s+1] - cu_kv[s], or with kv_lens min(kv_lens[s], that), at least 0.  For query head h, KV head h / (Hq/Hkv):
+ *     s_ij = softmax_scale * <Q_i, K_j>;  LSE_i = ln sum_j exp(s_ij);  O_i = sum_j exp(s_ij - LSE_i) V_j
+ * Rows of a sequence without valid keys get O = 0, LSE = -inf.  There is no causal mask and no position in it: for several
+ * queries of one request (draft tokens, beams of a search over the same states) let its sequence hold them all.
+ *
+ *   q, o             device, [total_q][Hq][d];  lse: float [Hq][total_q] (natural log)
+ *   k, v             device, [total_kv][Hkv][d]
+ *   cu_q, cu_kv      device int32[num_seqs+1], non-decreasing, within 0..total; rows in front of cu[0] and from cu[num_seqs] on
+ *                    belong to no sequence: they are not read, and left as they were in the outputs
+ *   kv_lens          device int32[num_seqs] or NULL: valid keys of a sequence, for padded caches (cu_kv then holds where each
+ *                    one's rows begin and end).  Rows behind the valid keys are not read, whatever they hold.
+ *   cu_q_host, cu_kv_host  host copies or NULL; when given they are checked (HYD_ERR_SEQLENS; HYD_ERR_SHAPE for a sequence above its
+ *                    bound, cu_kv only without kv_lens)
+ *   max_seqlen_q     bound on the queries of a sequence, 1..total_q;  max_seqlen_kv: on its valid keys, 0..total_kv.  Where a
+ *                    bound is too small, the results of that sequence are undefined, never an access outside the buffers.
+ *   head_dim         64 or 128; max_seqlen_q * Hq * head_dim and max_seqlen_kv * Hkv * head_dim elements stay below 2 GiB
+ *   workspace        device, 256-byte aligned, hyd_cross_attn_workspace_bytes(...) bytes.  A size never falls as total_q, total_kv,
+ *                    num_seqs or the bounds grow, so that one workspace serves every smaller call.
+ * Few rows (max_seqlen_q * Hq/Hkv up to 32) run a kernel of their own, bound by reading K and V once.
+ * T = 0 or num_seqs = 0 is a no-op.  Equal calls give equal bits.  Nothing depends on what the workspace held before.
+ */
+size_t hyd_cross_attn_workspace_bytes(int total_q, int total_kv, int num_seqs, int max_seqlen_q, int max_seqlen_kv,
+                                      int hq, int hkv, int head_dim, hyd_dtype dt, int is_bwd);
+
+hyd_status hyd_cross_attn_fwd(const void* q, const void* k, const void* v,
+                              const int32_t* cu_q, const int32_t* cu_kv, const int32_t* kv_lens, int num_seqs,
+                              const int32_t* cu_q_host, const int32_t* cu_kv_host,
+                              int total_q, int total_kv, int max_seqlen_q, int max_seqlen_kv,
+                              int hq, int hkv, int head_dim, float softmax_scale, hyd_dtype dt,
+                              void* o, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
  * Rotary positions in general form, for models whose heads, layouts or contexts hyd_rope_packed does not cover, and for
  * serving.  Pair p of a head, p in [0, rot_dim / 2), is (x[p], x[p + rot_dim / 2]) with HYD_ROPE_HALF and (x[2 p], x[2 p + 1])
  * with HYD_ROPE_INTERLEAVED.  At position m it becomes

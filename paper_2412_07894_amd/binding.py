@@ -20,6 +20,7 @@ EXPORTS = (
     "hyd_varlen_attn_fwd_noalloc", "hyd_varlen_attn_fwd_noalloc_max_workspace",
     "hyd_varlen_attn_schedule_status", "hyd_varlen_attn_schedule_layout",
     "hyd_varlen_attn_fwd_rope", "hyd_varlen_attn_bwd_rope", "hyd_rope_rotate", "hyd_rope_frequencies",
+    "hyd_cross_attn_workspace_bytes", "hyd_cross_attn_fwd",
 )
 RANGE_ALIGN = 256   # HYD_RANGE_ALIGN of the header
 ROPE_LAYOUTS = {"half": 0, "interleaved": 1}                  # hyd_rope_layout
@@ -75,6 +76,10 @@ def load():
     lib.hyd_attn_merge.argtypes = [vp, vp, vp, vp, i, i, i, i, vp, vp, vp]
     lib.hyd_rope_packed.restype = i
     lib.hyd_rope_packed.argtypes = [vp, ip, i, i, i, i, f, i, i, vp, vp]
+    lib.hyd_cross_attn_workspace_bytes.restype = sz
+    lib.hyd_cross_attn_workspace_bytes.argtypes = [i] * 10
+    lib.hyd_cross_attn_fwd.restype = i
+    lib.hyd_cross_attn_fwd.argtypes = [vp, vp, vp, ip, ip, ip, i, ip, ip, i, i, i, i, i, i, i, f, i, vp, vp, vp, sz, vp]
     l, dbl = ctypes.c_int64, ctypes.c_double
     lib.hyd_rope_rotate.restype = i
     lib.hyd_rope_rotate.argtypes = [vp, i, l, vp, l, vp, i, l, vp, l, ip, ip, i, ip, i, i, vp, i, i, f, i, i, vp]
@@ -303,6 +308,65 @@ def rope_packed(x, cu_seqlens, base=10000.0, inverse=False, out=None, stream=Non
     _check(load().hyd_rope_packed(x.data_ptr(), cu_seqlens.data_ptr(), cu_seqlens.numel() - 1, T, h, d, float(base),
                                   int(bool(inverse)), _dtype_code(x), out.data_ptr(), _stream_ptr(stream)))
     return out
+
+
+def cross_attn_workspace_bytes(total_q, total_kv, num_seqs, max_seqlen_q, max_seqlen_kv, hq, hkv, head_dim, dtype_code, is_bwd):
+    """Bytes of workspace of cross_attn_fwd (is_bwd false) or cross_attn_bwd; 0 for sizes that are refused."""
+    return int(load().hyd_cross_attn_workspace_bytes(total_q, total_kv, num_seqs, max_seqlen_q, max_seqlen_kv, hq, hkv, head_dim,
+                                                     dtype_code, int(bool(is_bwd))))
+
+
+def _like(name, t, shape, dtype, device):
+    """t as it is, checked; made if None."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {tuple(shape)} tensor of {dtype} on {device}, got {tuple(t.shape)} {t.dtype} {t.device}")
+    return t
+
+
+def _cross_sizes(q, k, v, cu_q, cu_kv, max_seqlen_q, max_seqlen_kv, workspace, is_bwd):
+    """Checks of the tensors that both directions take: (Tq, Tk, num_seqs, Hq, Hkv, d, dtype code, workspace)."""
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError(f"q and k must be [rows, heads, d], got {tuple(q.shape)} and {tuple(k.shape)}")
+    (Tq, hq, d), (Tk, hkv, _), dev = q.shape, k.shape, q.device
+    dt = _dtype_code(q)
+    _like("q", q, (Tq, hq, d), q.dtype, dev)
+    _like("k", k, (Tk, hkv, d), q.dtype, dev)
+    _like("v", v, (Tk, hkv, d), q.dtype, dev)
+    nseq = cu_q.numel() - 1
+    if nseq < 0 or cu_kv.numel() != nseq + 1:
+        raise ValueError(f"cu_q and cu_kv must have num_seqs + 1 elements, got {cu_q.numel()} and {cu_kv.numel()}")
+    if workspace is None:
+        workspace = _workspace(cross_attn_workspace_bytes(Tq, Tk, nseq, max_seqlen_q, max_seqlen_kv, hq, hkv, d, dt, is_bwd), dev)
+    elif workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.device != dev:
+        raise ValueError(f"workspace must be a contiguous uint8 tensor on {dev}, got {workspace.dtype} {workspace.device}")
+    return Tq, Tk, nseq, hq, hkv, d, dt, workspace
+
+
+def _host_lens(name, cu_host, nseq):
+    if cu_host is not None and len(cu_host) != nseq + 1:
+        raise ValueError(f"{name} must have num_seqs + 1 = {nseq + 1} elements, got {len(cu_host)}")
+    return _host_ptr(cu_host)
+
+
+def cross_attn_fwd(q, k, v, cu_q, cu_kv, max_seqlen_q, max_seqlen_kv, softmax_scale, kv_lens=None, cu_q_host=None, cu_kv_host=None,
+                   workspace=None, stream=None, out=None, lse=None):
+    """Cross attention of packed batches: queries q[Tq,Hq,d] of sequence s (rows cu_q[s]..cu_q[s+1]) on all its keys in k, v[Tk,Hkv,d]
+    (rows cu_kv[s]..cu_kv[s+1], of which kv_lens[s] are valid, all if kv_lens is None).  Returns (o[Tq,Hq,d], lse[Hq,Tq] fp32);
+    a sequence without valid keys gets o = 0, lse = -inf.  Work goes to `stream`, by default the current one of q's device."""
+    Tq, Tk, nseq, hq, hkv, d, dt, ws = _cross_sizes(q, k, v, cu_q, cu_kv, max_seqlen_q, max_seqlen_kv, workspace, False)
+    dev = q.device
+    o = _like("out", out, q.shape, q.dtype, dev)
+    lse = _like("lse", lse, (hq, Tq), torch.float32, dev)
+    kq, hp_q = _host_lens("cu_q_host", cu_q_host, nseq)
+    kk, hp_k = _host_lens("cu_kv_host", cu_kv_host, nseq)
+    with _on(dev):
+        _check(load().hyd_cross_attn_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), _int32("cu_q", cu_q, nseq + 1, dev),
+                                         _int32("cu_kv", cu_kv, nseq + 1, dev), _int32("kv_lens", kv_lens, nseq, dev), nseq, hp_q, hp_k,
+                                         Tq, Tk, int(max_seqlen_q), int(max_seqlen_kv), hq, hkv, d, float(softmax_scale), dt,
+                                         o.data_ptr(), lse.data_ptr(), ws.data_ptr(), ws.numel(), _stream_of(dev, stream)))
+    return o, lse
 
 
 def rope_frequencies(rot_dim, base=10000.0, scaling="plain", factor=1.0, original_length=0.0, low=1.0, high=32.0, device="cuda"):

@@ -8,7 +8,7 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libhyd_attn.so")
-SOURCES = [os.path.join(CSRC, f) for f in ("hyd_api.hip", "hyd_rotary.hip", "hyd_plan.cpp")]
+SOURCES = [os.path.join(CSRC, f) for f in ("hyd_api.hip", "hyd_cross.hip", "hyd_rotary.hip", "hyd_plan.cpp")]
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

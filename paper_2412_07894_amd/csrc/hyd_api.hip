@@ -18,6 +18,21 @@
 #include "hyd_merge.h"
 #include "hyd_rope.h"
 
+namespace hyd {
+
+// One list per workgroup: blockIdx.x = 0: tile0 -> sv0, blockIdx.x = 1: tile1 -> sv1.  With rope_tab != NULL the
+// first workgroup also fills the rotary frequency table of the call (half_d entries, see hyd_rope_regs.h).
+__global__ void __launch_bounds__(kPreludeThreads) hyd_schedule_prelude(const int32_t* __restrict__ cu, int nseq, int T,
+                                                                       int tile0, SchedView sv0, int tile1, SchedView sv1,
+                                                                       double* rope_tab, int half_d, double log2_base) {
+    extern __shared__ int lds_lev[];
+    if (rope_tab && blockIdx.x == 0) rope_table_fill(rope_tab, half_d, log2_base, threadIdx.x, kPreludeThreads);
+    const bool second = blockIdx.x != 0;
+    build_schedule(cu, nseq, T, second ? tile1 : tile0, second ? sv1 : sv0, lds_lev, kPreludeThreads);
+}
+
+}  // namespace hyd
+
 namespace {
 
 using namespace hyd;
@@ -255,27 +270,6 @@ WsLayout bwd_layout(int T, int nseq, int hq, int hkv, int head_dim, hyd_dtype dt
 }
 
 bool head_dim_ok(hyd_dtype dt, int d) { (void)dt; return d == 64 || d == 128; }
-
-// Spread of (item, head) pairs over the 8 queues: whole KV groups per queue when the KV heads
-// divide over the queues, else single heads, else items striped with all heads in every queue.
-// `hq` counts the query heads in units of an item's heads.
-HeadMap head_map_q(int hq, int hkv, int grid) {
-    HeadMap hm;
-    hm.grid = grid;
-    hm.heads = hq;
-    if (hkv % kQueues == 0) { hm.striped = 0; hm.hpq = hq / kQueues; hm.group = hq / hkv; }
-    else if (hq % kQueues == 0) { hm.striped = 0; hm.hpq = hq / kQueues; hm.group = 1; }
-    else { hm.striped = 1; hm.hpq = hq; hm.group = 1; }
-    return hm;
-}
-HeadMap head_map_kv(int hkv, int grid) {
-    HeadMap hm;
-    hm.grid = grid;
-    hm.heads = hkv;
-    if (hkv % kQueues == 0) { hm.striped = 0; hm.hpq = hkv / kQueues; hm.group = 1; }
-    else { hm.striped = 1; hm.hpq = hkv; hm.group = 1; }
-    return hm;
-}
 
 hyd_status validate_common(const int32_t* cu, int num_seqs, const int32_t* cu_host, int T,
                            int max_seqlen, int hq, int hkv, int head_dim, hyd_dtype dt,

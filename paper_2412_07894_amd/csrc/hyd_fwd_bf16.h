@@ -99,7 +99,8 @@ __device__ __forceinline__ uint32_t largest_bits(const f32x16 (&a)[N]) {
 // join); only the masking itself sits in a wave-uniform branch.  `diag`: this is the wave's
 // diagonal tile (its second 32-key block may be hidden altogether).
 // D: head dimension (128 or 64): D/16 contraction steps in the score product, D/32 output blocks.
-template <int D>
+// kExact: the row sum is that of the probabilities as they are, not rounded (LSE to fp32 accuracy).
+template <int D, bool kExact = false>
 __device__ __forceinline__ void fwd_tile(int Kt, int Vt, const FragAddr& fa, const bf16x8 (&qf)[D / 16],
                                          f32x16 (&acc_o)[D / 32], float& m_ref, float& l_run, float scale_log2,
                                          int koff, bool diag, int t, int& t_find, bool& overflow) {
@@ -182,6 +183,10 @@ __device__ __forceinline__ void fwd_tile(int Kt, int Vt, const FragAddr& fa, con
         const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][r], scale_log2, -m_ref));
         const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][r + 1], scale_log2, -m_ref));
         const uint32_t pair = pack_bf16(p0, p1);
+        if constexpr (kExact) {
+            lsum += p0 + p1;
+            return pair;
+        }
         // row sum of the ROUNDED probabilities (what the P V product actually uses)
         bf16x2 pr;
         __builtin_memcpy(&pr, &pair, 4);

@@ -75,6 +75,27 @@ struct HeadMap {              // how (item, head) pairs are spread over the queu
     int grid;                 // workgroups of the launch
 };
 
+// Spread of (item, head) pairs over the 8 queues: whole KV groups per queue when the KV heads
+// divide over the queues, else single heads, else items striped with all heads in every queue.
+// `hq` counts the query heads in units of an item's heads.
+inline HeadMap head_map_q(int hq, int hkv, int grid) {
+    HeadMap hm;
+    hm.grid = grid;
+    hm.heads = hq;
+    if (hkv % kQueues == 0) { hm.striped = 0; hm.hpq = hq / kQueues; hm.group = hq / hkv; }
+    else if (hq % kQueues == 0) { hm.striped = 0; hm.hpq = hq / kQueues; hm.group = 1; }
+    else { hm.striped = 1; hm.hpq = hq; hm.group = 1; }
+    return hm;
+}
+inline HeadMap head_map_kv(int hkv, int grid) {
+    HeadMap hm;
+    hm.grid = grid;
+    hm.heads = hkv;
+    if (hkv % kQueues == 0) { hm.striped = 0; hm.hpq = hkv / kQueues; hm.group = 1; }
+    else { hm.striped = 1; hm.hpq = hkv; hm.group = 1; }
+    return hm;
+}
+
 // In-place inclusive scan of v[0..n) by ONE wave (all 64 lanes call it; n arbitrary): every lane
 // sums a contiguous chunk, the chunk sums are scanned across the lanes, each lane rewrites its chunk.
 __device__ __forceinline__ void wave_inclusive_scan(int* v, int n, int lane) {
@@ -224,17 +245,6 @@ __device__ __forceinline__ void build_schedule(const int32_t* __restrict__ cu, i
             *reinterpret_cast<i32x4*>(sv.exec + 4 * e) = rec;
         }
     }
-}
-
-// One list per workgroup: blockIdx.x = 0: tile0 -> sv0, blockIdx.x = 1: tile1 -> sv1.  With rope_tab != NULL the
-// first workgroup also fills the rotary frequency table of the call (half_d entries, see hyd_rope_regs.h).
-__global__ void __launch_bounds__(kPreludeThreads) hyd_schedule_prelude(const int32_t* __restrict__ cu, int nseq, int T,
-                                                                       int tile0, SchedView sv0, int tile1, SchedView sv1,
-                                                                       double* rope_tab, int half_d, double log2_base) {
-    extern __shared__ int lds_lev[];
-    if (rope_tab && blockIdx.x == 0) rope_table_fill(rope_tab, half_d, log2_base, threadIdx.x, kPreludeThreads);
-    const bool second = blockIdx.x != 0;
-    build_schedule(cu, nseq, T, second ? tile1 : tile0, second ? sv1 : sv0, lds_lev, kPreludeThreads);
 }
 
 // Query side of an item of the bf16 forward and dQ kernels, 32 rows of a head per wave; rows = 256 >> S.
