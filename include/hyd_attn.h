@@ -354,6 +354,21 @@ hyd_status hyd_cross_attn_fwd(const void* q, const void* k, const void* v,
                               void* o, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /*
+ * Backward of the above.  o and lse are the forward's results; with P_ij = exp(s_ij - LSE_i), D_i = <dO_i, O_i> and
+ * dS_ij = P_ij (<dO_i, V_j> - D_i)
+ *     dQ_i = scale sum_j dS_ij K_j;  dK_j = scale sum_{h in group, i} dS_ij Q_i;  dV_j = sum_{h in group, i} P_ij dO_i
+ * dk and dv are written for every row of a sequence, zeros behind its valid keys; dq is 0 where there are none.  Rows that belong to
+ * no sequence are neither read nor written.  Arithmetic, and the ranges of values it asks for, as hyd_varlen_attn_bwd.
+ * total_q = 0 or total_kv = 0 alone is not a no-op: the other side's gradients are zeros.
+ */
+hyd_status hyd_cross_attn_bwd(const void* q, const void* k, const void* v, const void* o, const float* lse, const void* d_o,
+                              const int32_t* cu_q, const int32_t* cu_kv, const int32_t* kv_lens, int num_seqs,
+                              const int32_t* cu_q_host, const int32_t* cu_kv_host,
+                              int total_q, int total_kv, int max_seqlen_q, int max_seqlen_kv,
+                              int hq, int hkv, int head_dim, float softmax_scale, hyd_dtype dt,
+                              void* dq, void* dk, void* dv, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
  * Rotary positions in general form, for models whose heads, layouts or contexts hyd_rope_packed does not cover, and for
  * serving.  Pair p of a head, p in [0, rot_dim / 2), is (x[p], x[p + rot_dim / 2]) with HYD_ROPE_HALF and (x[2 p], x[2 p + 1])
  * with HYD_ROPE_INTERLEAVED.  At position m it becomes

@@ -20,7 +20,7 @@ EXPORTS = (
     "hyd_varlen_attn_fwd_noalloc", "hyd_varlen_attn_fwd_noalloc_max_workspace",
     "hyd_varlen_attn_schedule_status", "hyd_varlen_attn_schedule_layout",
     "hyd_varlen_attn_fwd_rope", "hyd_varlen_attn_bwd_rope", "hyd_rope_rotate", "hyd_rope_frequencies",
-    "hyd_cross_attn_workspace_bytes", "hyd_cross_attn_fwd",
+    "hyd_cross_attn_workspace_bytes", "hyd_cross_attn_fwd", "hyd_cross_attn_bwd",
 )
 RANGE_ALIGN = 256   # HYD_RANGE_ALIGN of the header
 ROPE_LAYOUTS = {"half": 0, "interleaved": 1}                  # hyd_rope_layout
@@ -80,6 +80,8 @@ def load():
     lib.hyd_cross_attn_workspace_bytes.argtypes = [i] * 10
     lib.hyd_cross_attn_fwd.restype = i
     lib.hyd_cross_attn_fwd.argtypes = [vp, vp, vp, ip, ip, ip, i, ip, ip, i, i, i, i, i, i, i, f, i, vp, vp, vp, sz, vp]
+    lib.hyd_cross_attn_bwd.restype = i
+    lib.hyd_cross_attn_bwd.argtypes = [vp, vp, vp, vp, vp, vp, ip, ip, ip, i, ip, ip, i, i, i, i, i, i, i, f, i, vp, vp, vp, vp, sz, vp]
     l, dbl = ctypes.c_int64, ctypes.c_double
     lib.hyd_rope_rotate.restype = i
     lib.hyd_rope_rotate.argtypes = [vp, i, l, vp, l, vp, i, l, vp, l, ip, ip, i, ip, i, i, vp, i, i, f, i, i, vp]
@@ -367,6 +369,29 @@ def cross_attn_fwd(q, k, v, cu_q, cu_kv, max_seqlen_q, max_seqlen_kv, softmax_sc
                                          Tq, Tk, int(max_seqlen_q), int(max_seqlen_kv), hq, hkv, d, float(softmax_scale), dt,
                                          o.data_ptr(), lse.data_ptr(), ws.data_ptr(), ws.numel(), _stream_of(dev, stream)))
     return o, lse
+
+
+def cross_attn_bwd(q, k, v, o, lse, d_o, cu_q, cu_kv, max_seqlen_q, max_seqlen_kv, softmax_scale, kv_lens=None, cu_q_host=None,
+                   cu_kv_host=None, workspace=None, stream=None, dq=None, dk=None, dv=None):
+    """Gradients (dq, dk, dv) of cross_attn_fwd for an upstream gradient d_o of o; o and lse are the forward's results.  Rows of dk
+    and dv behind a sequence's valid keys are zeros."""
+    Tq, Tk, nseq, hq, hkv, d, dt, ws = _cross_sizes(q, k, v, cu_q, cu_kv, max_seqlen_q, max_seqlen_kv, workspace, True)
+    dev = q.device
+    _like("o", o, q.shape, q.dtype, dev)
+    _like("d_o", d_o, q.shape, q.dtype, dev)
+    _like("lse", lse, (hq, Tq), torch.float32, dev)
+    dq = _like("dq", dq, q.shape, q.dtype, dev)
+    dk = _like("dk", dk, k.shape, k.dtype, dev)
+    dv = _like("dv", dv, v.shape, v.dtype, dev)
+    kq, hp_q = _host_lens("cu_q_host", cu_q_host, nseq)
+    kk, hp_k = _host_lens("cu_kv_host", cu_kv_host, nseq)
+    with _on(dev):
+        _check(load().hyd_cross_attn_bwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), d_o.data_ptr(),
+                                         _int32("cu_q", cu_q, nseq + 1, dev), _int32("cu_kv", cu_kv, nseq + 1, dev),
+                                         _int32("kv_lens", kv_lens, nseq, dev), nseq, hp_q, hp_k, Tq, Tk, int(max_seqlen_q),
+                                         int(max_seqlen_kv), hq, hkv, d, float(softmax_scale), dt, dq.data_ptr(), dk.data_ptr(),
+                                         dv.data_ptr(), ws.data_ptr(), ws.numel(), _stream_of(dev, stream)))
+    return dq, dk, dv
 
 
 def rope_frequencies(rot_dim, base=10000.0, scaling="plain", factor=1.0, original_length=0.0, low=1.0, high=32.0, device="cuda"):

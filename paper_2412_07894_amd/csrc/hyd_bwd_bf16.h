@@ -257,6 +257,9 @@ struct BwdParams {
                                       // (the fp16 copy it writes is the rotated Q) and turns dQ back before writing it
 };
 
+// Cross attention: T counts the packed rows of a KV head, planes of partial sums have part_rows rows.
+struct CrossBwdParams : BwdParams { int part_rows; };
+
 // The records of a tile kernel and how they are shared out.
 struct WorkList { const int* hdr; int* cursors; const int* items; HeadMap hm; };
 

@@ -29,6 +29,7 @@ constexpr int kKwStageBytes = 2 * kKwTileBytes;                       // Q, dO
 constexpr int kKwStatOff = kKwStages * kKwStageBytes;                 // [stage][LSE2, D][64]
 constexpr int kKwSlotOff = kKwStatOff + kKwStages * 2 * kKwBM * 4;
 constexpr int kKwVOff = 3 * kKwStageBytes;                            // V rows while an item begins
+constexpr int kXPartShift = 16;
 constexpr int kKwLds = kKwVOff + kKwBN * kRowBytes;                   // 160 KB: all of a CU's LDS
 static_assert(kKwSlotOff + 64 <= kKwLds, "statistics and work slot lie behind the ring");
 
@@ -75,8 +76,11 @@ __device__ __forceinline__ void keep_acc(f32x16 (&a)[2][N], f32x16 (&b)[2][N]) {
     for (int i = 0; i < 2 * N; ++i) asm volatile("" : "+a"(a[i / N][i % N]), "+a"(b[i / N][i % N]));
 }
 
-template <int D = kHeadDim>
-__global__ void __launch_bounds__(kKwThreads, 1) hyd_bwd_dkdv_wide_bf16_kernel(BwdParams p, WorkList list) {
+// With CrossBwdParams: cross attention (hyd_cross_bwd.h).  The rows of a KV head's query heads are one run of p.T packed rows, every key sees all rows
+// of its sequence, a record names the item's keys, its part and its rows (CrossList), and an item may be taken in p.part_max parts.
+template <int D = kHeadDim, typename Params = BwdParams>
+__global__ void __launch_bounds__(kKwThreads, 1) hyd_bwd_dkdv_wide_bf16_kernel(Params p, WorkList list) {
+    constexpr bool X = std::is_same<Params, CrossBwdParams>::value;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     static_assert(D == 128 || D == 64, "head dimension");
     constexpr int kRowB = D * 2, NK = D / 16, NDB = D / 32;
@@ -84,8 +88,8 @@ __global__ void __launch_bounds__(kKwThreads, 1) hyd_bwd_dkdv_wide_bf16_kernel(B
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, half = lane >> 5;
-    const int G = p.hq / p.hkv;
-    const int64_t q_stride = (int64_t)p.hq * D, kv_stride = (int64_t)p.hkv * D;
+    const int G = X ? 1 : p.hq / p.hkv;
+    const int64_t q_stride = X ? D : (int64_t)p.hq * D, kv_stride = (int64_t)p.hkv * D;
     const uint32_t q_stride_b = (uint32_t)q_stride * 2, kv_stride_b = (uint32_t)kv_stride * 2;
     const unsigned long long t_start = p.tr.rec ? wall_clock64() : 0ull;
     unsigned long long n_done = 0;
@@ -118,15 +122,18 @@ __global__ void __launch_bounds__(kKwThreads, 1) hyd_bwd_dkdv_wide_bf16_kernel(B
         __syncthreads();                                      // everybody has read the work slot: its bytes may be overwritten
         const int lev = wi.lev, g = wi.head, row0 = wi.row0, L = wi.len;
         const int n_tiles = (L + kKwBN - 1) / kKwBN;
-        const int j0 = (n_tiles - lev) * kKwBN;
-        n_done += (min(L - j0, kKwBN) + kKvBN - 1) / kKvBN;   // (the trace counts tiles of the list of whole tiles)
+        const int part = X ? lev >> kXPartShift : 0, per_part = X ? (((L + kKwBM - 1) / kKwBM) + p.part_max - 1) / p.part_max : 0;
+        const int j0 = X ? 0 : (n_tiles - lev) * kKwBN;
+        const int kv0 = wi.seq;                               // (X: first key row of the item in K and V)
+        const int Lk = X ? lev & ((1 << kXPartShift) - 1) : L;        // keys end here, counted as j0 and wkey0 are
+        if (!X) n_done += (min(L - j0, kKwBN) + kKvBN - 1) / kKvBN;   // (the trace counts tiles of the list of whole tiles)
         const int wkey0 = j0 + 64 * wave;                     // first key of this wave
-        const bool active = wkey0 < L;
+        const bool active = wkey0 < Lk;
         const int td = wkey0 / kKwBM;                         // query tile that holds the wave's diagonal
-        const int qt_first = j0 / kKwBM;
-        const int n_qt = (L + kKwBM - 1) / kKwBM - qt_first;
+        const int qt_first = X ? part * per_part : j0 / kKwBM;
+        const int n_qt = X ? max(min((L + kKwBM - 1) / kKwBM - qt_first, per_part), 0) : (L + kKwBM - 1) / kKwBM - qt_first;
         const int n_iter = n_qt * G;
-        const uint32_t q_bytes = (uint32_t)(L - 1) * q_stride_b + kRowB;
+        const uint32_t q_bytes = X && L == 0 ? 0 : (uint32_t)(L - 1) * q_stride_b + kRowB;
         const uint32_t stat_bytes = (uint32_t)L * 4;
 
         constexpr int kDmaPerStage = 2 * (16 / kKwWaves) + 1;
@@ -135,7 +142,7 @@ __global__ void __launch_bounds__(kKwThreads, 1) hyd_bwd_dkdv_wide_bf16_kernel(B
         auto dma_stage = [&](int stage, bool stats) {
             const int h = g * G + ld_h, qt = ld_qt;
             if (++ld_h == G) { ld_h = 0; ++ld_qt; }
-            const int64_t base = (int64_t)row0 * q_stride + (int64_t)h * D;
+            const int64_t base = X ? ((int64_t)h * p.T + row0) * D : (int64_t)row0 * q_stride + (int64_t)h * D;
             const __amdgpu_buffer_rsrc_t rq = make_rsrc(p.sc.q16 + base, q_bytes);
             const __amdgpu_buffer_rsrc_t rdo = make_rsrc(p.sc.do16 + base, q_bytes);
             char* dst = smem + stage * kKwStageBytes + 4 * wave * kRowBytes;
@@ -163,8 +170,8 @@ __global__ void __launch_bounds__(kKwThreads, 1) hyd_bwd_dkdv_wide_bf16_kernel(B
             dma_stage(0, false);
         }
         {
-            const uint32_t k_bytes = (uint32_t)(min(L - j0, kKwBN) - 1) * kv_stride_b + kRowB;
-            const int64_t off = (int64_t)(row0 + j0) * kv_stride + (int64_t)g * D;
+            const uint32_t k_bytes = (uint32_t)(min(Lk - j0, kKwBN) - 1) * kv_stride_b + kRowB;
+            const int64_t off = (int64_t)(X ? kv0 : row0 + j0) * kv_stride + (int64_t)g * D;
             auto tile_at = [&](int j) { return (uint32_t)(64 * j) * kv_stride_b; };
             dma_rows<kKwWaves>(make_rsrc(p.sc.k16 + off, k_bytes), smem + kKwStageBytes, [](int j) { return j * kKwTileBytes; },
                                kKwBN / 64, kv_stride_b, tile_at, wave, dma_voff_kv);
@@ -365,8 +372,8 @@ __global__ void __launch_bounds__(kKwThreads, 1) hyd_bwd_dkdv_wide_bf16_kernel(B
         };
         // Three loops: tiles before the wave's keys, the tile of its diagonal, the others.  One loop with a choice of bodies
         // would have the accumulators meet in vector registers; so they stay in their file from one to the next.
-        const int skip = active ? min(max(td - qt_first, 0) * G, n_iter) : n_iter;
-        const int diag = active ? min(max(td + 1 - qt_first, 0) * G, n_iter) : n_iter;
+        const int skip = active ? (X ? 0 : min(max(td - qt_first, 0) * G, n_iter)) : n_iter;
+        const int diag = active ? (X ? 0 : min(max(td + 1 - qt_first, 0) * G, n_iter)) : n_iter;
         while (it < skip) { turn(); advance(); }
         if (it < n_iter) {
 #pragma unroll
@@ -378,7 +385,7 @@ __global__ void __launch_bounds__(kKwThreads, 1) hyd_bwd_dkdv_wide_bf16_kernel(B
             }
         }
         keep_acc(dv, dk);
-        while (it < diag) {
+        while (!X && it < diag) {
             block(std::integral_constant<int, 1>{}, std::true_type{}, 0, fa_row);
             turn();
             block(std::integral_constant<int, 2>{}, std::true_type{}, 1, fa_row + move_of());
@@ -399,16 +406,24 @@ __global__ void __launch_bounds__(kKwThreads, 1) hyd_bwd_dkdv_wide_bf16_kernel(B
             const uint32_t o_stage = lds0 + (uint32_t)(wave * 3 * 32 * kRowBytes);      // this wave's 24 KB of the ring
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
-                if (wkey0 + 32 * kb < L) {
-                    const int64_t out = (int64_t)(row0 + wkey0 + 32 * kb) * kv_stride + (int64_t)g * D;
-                    store_rows_via_lds<D>(p.dv + out, kv_stride, L - wkey0 - 32 * kb, dv[kb], unscale, o_stage, lane);
-                    store_rows_via_lds<D>(p.dk + out, kv_stride, L - wkey0 - 32 * kb, dk[kb], p.scale * unscale, o_stage + 32 * kRowBytes, lane);
+                if (wkey0 + 32 * kb < Lk) {
+                    const int64_t out = (int64_t)((X ? kv0 : row0) + wkey0 + 32 * kb) * kv_stride + (int64_t)g * D;
+                    if constexpr (X) {
+                        if (p.part_max > 1) {
+                            const int64_t plane = (int64_t)p.part_rows * kv_stride;
+                            store_rows_f32_via_lds<D>(p.part + (p.part_max + part) * plane + out, kv_stride, Lk - wkey0 - 32 * kb, dv[kb], unscale, o_stage, lane);
+                            store_rows_f32_via_lds<D>(p.part + part * plane + out, kv_stride, Lk - wkey0 - 32 * kb, dk[kb], p.scale * unscale, o_stage + 32 * kRowBytes, lane);
+                            continue;
+                        }
+                    }
+                    store_rows_via_lds<D>(p.dv + out, kv_stride, Lk - wkey0 - 32 * kb, dv[kb], unscale, o_stage, lane);
+                    store_rows_via_lds<D>(p.dk + out, kv_stride, Lk - wkey0 - 32 * kb, dk[kb], p.scale * unscale, o_stage + 32 * kRowBytes, lane);
                 }
             }
         }
         have = wf.next(list.hm, list.cursors, list.items, slot, wi);
     }
-    if (p.tr.rec && *list.hdr > 0) trace_write(p.tr, 1, t_start, n_done);       // (a list may be left to the other form)
+    if (!X && p.tr.rec && *list.hdr > 0) trace_write(p.tr, 1, t_start, n_done);       // (a list may be left to the other form)
 }
 
 }  // namespace hyd

@@ -112,7 +112,7 @@ __global__ void __launch_bounds__(kPreludeThreads) hyd_cross_list_kernel(CrossSh
 struct CrossRows {
     int G;
     float inv;
-    __device__ __forceinline__ void init(int g) { G = g; inv = 1.f / (float)g; }
+    __device__ __forceinline__ void init(int g) { G = g; inv = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(1.f / (float)g))); }
     __device__ __forceinline__ void split(int r, int& token, int& head) const {
         token = (int)(((float)r + 0.5f) * inv);
         head = r - token * G;

@@ -3,6 +3,7 @@
 
 #include <mutex>
 
+#include "hyd_cross_bwd.h"
 #include "hyd_cross_fwd.h"
 #include "hyd_host.h"
 
@@ -75,6 +76,42 @@ int parts_in_room(const FwdLayout& w, const Sizes& z, size_t bytes, int want) {
     return want;
 }
 
+// ---- backward
+constexpr int kBwdMaxParts = 16, kDqPartRows = 65536, kKvPartRows = 131072, kBwdItems = 512;
+struct BwdLayout { size_t q_hdr, q_items, kv_hdr, kv_items, stat[4], q16, do16, k16, absmax, need, total; long long n_q, n_kv; };
+BwdLayout bwd_layout(const Sizes& z) {
+    BwdLayout w;
+    const int G = z.hq / z.hkv;
+    w.n_q = most_tiles((long long)z.Tq * G, (long long)z.max_q * G, z.nseq, kDqBM);
+    w.n_kv = most_tiles(z.Tk, z.max_kv, z.nseq, kKwBN);
+    const size_t q_elems = (size_t)z.Tq * z.hq * z.d, kv_elems = (size_t)z.Tk * z.hkv * z.d;
+    const auto records = [](long long n) { return align_up(16 * (size_t)(n > kBwdItems ? n : kBwdItems)); };      // (parts: kBwdItems records at most)
+    size_t at = 0;
+    w.q_hdr = at;    at += align_up(sizeof(int) * kHdrTotal);
+    w.q_items = at;  at += records(w.n_q);
+    w.kv_hdr = at;   at += align_up(sizeof(int) * kHdrTotal);
+    w.kv_items = at; at += records(w.n_kv);
+    for (size_t& s : w.stat) { s = at; at += align_up(sizeof(float) * (size_t)z.Tq * z.hq); }
+    w.q16 = at;      at += align_up(2 * q_elems);
+    w.do16 = at;     at += align_up(2 * q_elems);
+    w.k16 = at;      at += align_up(2 * kv_elems);
+    w.absmax = at;   at += align_up(sizeof(uint32_t) * kPrepMaxWg);
+    w.need = at;
+    const size_t q_rows = (size_t)z.Tq * z.hq * kBwdMaxParts, kv_rows = (size_t)z.Tk * z.hkv * kBwdMaxParts;
+    const size_t dq = (q_rows < kDqPartRows ? q_rows : kDqPartRows) * (size_t)z.d * 4, dkv = (kv_rows < kKvPartRows ? kv_rows : kKvPartRows) * (size_t)z.d * 8;
+    w.total = at + align_up(dq > dkv ? dq : dkv);
+    return w;
+}
+// Parts of an item where `items` of them leave workgroups idle: up to `target` in all, none shorter than `least` of its `steps`, and as
+// many as their sums of `row_bytes` have room for (most_rows of `rows` at most).
+int bwd_parts(long long items, int target, long long steps, int least, size_t rows, size_t most_rows, size_t row_bytes, size_t room) {
+    long long n = items > 0 ? target / items : 1;
+    if (n > steps / least) n = steps / least;
+    if (n > kBwdMaxParts) n = kBwdMaxParts;
+    while (n > 1 && ((size_t)n * rows > most_rows || (size_t)n * rows * row_bytes > room)) --n;
+    return n > 1 ? (int)n : 1;
+}
+
 // ---- per-device state
 struct CrossDevice { bool ready = false, ok = false; };
 CrossDevice g_cross[64];
@@ -87,7 +124,8 @@ bool allow_lds(K kernel, int lds) {
 template <int D>
 bool prep_kernels() {
     return allow_lds(hyd_cross_fwd_bf16_kernel<D, false>, kFwdLds) && allow_lds(hyd_cross_fwd_bf16_kernel<D, true>, kFwdLds) &&
-           allow_lds(hyd_cross_few_bf16_kernel<D>, kFewLds);
+           allow_lds(hyd_cross_few_bf16_kernel<D>, kFewLds) && allow_lds(hyd_cross_dq_bf16_kernel<D>, kDqLds) &&
+           allow_lds(hyd_bwd_dkdv_wide_bf16_kernel<D, CrossBwdParams>, kKwLds);
 }
 hyd_status cross_device(int* cus) {
     int dev = 0;
@@ -178,6 +216,91 @@ void launch_fwd(const Sizes& z, const CrossShape& c, const void* q, const void* 
     }
 }
 
+template <int D>
+void launch_sum(const CrossSum& x, hipStream_t st) {
+    KernelTimer kt("cross_sum", st);
+    hipLaunchKernelGGL(hyd_cross_sum_kernel<D>, dim3((unsigned)x.T), dim3(kCrossSumThreads), 0, st, x);
+}
+
+struct BwdArgs { const void *q, *k, *v, *o; const float* lse; const void* d_o; void *dq, *dk, *dv; };
+template <int D>
+void launch_bwd(const Sizes& z, const CrossShape& c, const BwdArgs& a, float scale, char* ws, size_t ws_bytes, int cus, hipStream_t st) {
+    const BwdLayout w = bwd_layout(z);
+    const int G = c.G;
+    BwdScratch sc;
+    sc.Dq = reinterpret_cast<float*>(ws + w.stat[0]); sc.kqmul = reinterpret_cast<float*>(ws + w.stat[1]);
+    sc.lse2 = reinterpret_cast<float*>(ws + w.stat[2]); sc.Dkv = reinterpret_cast<float*>(ws + w.stat[3]);
+    sc.q16 = reinterpret_cast<uint16_t*>(ws + w.q16); sc.do16 = reinterpret_cast<uint16_t*>(ws + w.do16); sc.k16 = reinterpret_cast<uint16_t*>(ws + w.k16);
+    sc.absmax = reinterpret_cast<uint32_t*>(ws + w.absmax);
+    float* part = reinterpret_cast<float*>(ws + w.need);
+    const size_t room = ws_bytes - w.need, q_rows = (size_t)z.Tq * z.hq, kv_rows = (size_t)z.Tk * z.hkv;
+    const int parts_q = bwd_parts(w.n_q * z.hkv, kCus, tiles(z.max_kv, kDqBN), 8, q_rows, kDqPartRows, (size_t)D * 4, room);
+    const int parts_kv = bwd_parts(w.n_kv * z.hkv, kBwdItems, tiles((long long)z.max_q * G, kKwBM), 8, kv_rows, kKvPartRows, (size_t)D * 8, room);
+    int* q_hdr = reinterpret_cast<int*>(ws + w.q_hdr); int* kv_hdr = reinterpret_cast<int*>(ws + w.kv_hdr);
+    int* q_items = reinterpret_cast<int*>(ws + w.q_items); int* kv_items = reinterpret_cast<int*>(ws + w.kv_items);
+    const long long work_q = w.n_q * z.hkv * parts_q, work_kv = w.n_kv * z.hkv * parts_kv;
+    {
+        CrossPrepParams p;
+        p.c = c;
+        p.o = static_cast<const uint16_t*>(a.o); p.d_o = static_cast<const uint16_t*>(a.d_o); p.lse = a.lse; p.k = static_cast<const uint16_t*>(a.k);
+        p.dk = static_cast<uint16_t*>(a.dk); p.dv = static_cast<uint16_t*>(a.dv);
+        p.tok = prep_tokens(z.Tq, z.hq);
+        p.n_q = sc.n_absmax = prep_workgroups(z.Tq, p.tok);
+        p.sc = sc;
+        p.n_zero = !c.kv_lens ? 0 : (z.nseq < kCus ? z.nseq : kCus);
+        const long long copies = tiles((long long)z.Tk * z.hkv, 4 * kPrepThreads / (D / 8));
+        const int n_k = (int)(copies < kPrepTarget ? copies : kPrepTarget);
+        p.lists[0] = CrossList{q_hdr, q_items, kDqBM, parts_q, (int)(w.n_q * parts_q), false};
+        p.lists[1] = CrossList{kv_hdr, kv_items, kKwBN, parts_kv, (int)(w.n_kv * parts_kv), true};
+        KernelTimer kt("cross_prep", st);
+        hipLaunchKernelGGL(hyd_cross_prep_bf16_kernel<D>, dim3((unsigned)(kCrossLists + p.n_zero + p.n_q + n_k)), dim3(kPrepThreads), cross_prep_lds(z.hq, p.tok), st, p);
+    }
+    const auto grid_of = [&](long long work) { return (int)(work < 1 ? 1 : (work < cus ? work : cus)); };
+    {
+        CrossDqParams p;
+        p.c = c;
+        p.q = static_cast<const uint16_t*>(a.q); p.v = static_cast<const uint16_t*>(a.v); p.d_o = static_cast<const uint16_t*>(a.d_o);
+        p.sc = sc; p.dq = static_cast<uint16_t*>(a.dq);
+        p.part = part; p.parts = parts_q; p.scale = scale; p.scale_log2 = scale * kLog2eHost;
+        const int grid = grid_of(work_q);
+        const WorkList l{q_hdr, q_hdr + kHdrCursor, q_items, head_map_kv(z.hkv, grid)};
+        KernelTimer kt("cross_dq", st);
+        hipLaunchKernelGGL(hyd_cross_dq_bf16_kernel<D>, dim3(grid), dim3(kDqThreads), kDqLds, st, p, l);
+    }
+    if (parts_q > 1) launch_sum<D>(CrossSum{part, static_cast<uint16_t*>(a.dq), c.cu_q, nullptr, z.nseq, z.Tq, z.hq, parts_q}, st);
+    if (z.Tk == 0) return;
+    {
+        CrossBwdParams p;
+        memset(&p, 0, sizeof(p));
+        p.v = static_cast<const uint16_t*>(a.v);
+        p.sc = sc;
+        p.dk = static_cast<uint16_t*>(a.dk); p.dv = static_cast<uint16_t*>(a.dv);
+        p.T = z.Tq * G; p.hq = z.hkv; p.hkv = z.hkv;
+        p.scale = scale; p.scale_log2 = scale * kLog2eHost;
+        p.part = part; p.part_max = parts_kv; p.part_rows = z.Tk;
+        const int grid = grid_of(work_kv);
+        const WorkList l{kv_hdr, kv_hdr + kHdrCursor, kv_items, head_map_kv(z.hkv, grid)};
+        KernelTimer kt("cross_dkdv", st);
+        hipLaunchKernelGGL((hyd_bwd_dkdv_wide_bf16_kernel<D, CrossBwdParams>), dim3(grid), dim3(kKwThreads), kKwLds, st, p, l);
+    }
+    if (parts_kv > 1)
+        for (int which = 0; which < 2; ++which)
+            launch_sum<D>(CrossSum{part + (size_t)which * parts_kv * kv_rows * D, static_cast<uint16_t*>(which ? a.dv : a.dk), c.cu_kv, c.kv_lens, z.nseq, z.Tk, z.hkv, parts_kv}, st);
+}
+
+// What both directions check before any HIP call; HYD_OK with *nothing set: there is nothing to do.
+hyd_status check_call(const Sizes& z, const int32_t* cu_q, const int32_t* cu_kv, const int32_t* kv_lens, const int32_t* cu_q_host,
+                      const int32_t* cu_kv_host, bool pointers, const void* workspace, size_t bytes, size_t need, bool* nothing) {
+    *nothing = (z.Tq == 0 && z.Tk == 0) || z.nseq == 0;
+    if (*nothing) return HYD_OK;
+    if (z.Tq > 0 && z.max_q == 0) return HYD_ERR_SHAPE;
+    if (!cu_q || !cu_kv || !pointers) return HYD_ERR_NULL;
+    hyd_status st = check_lengths(cu_q_host, z.nseq, z.Tq, z.max_q, true);
+    if (st == HYD_OK) st = check_lengths(cu_kv_host, z.nseq, z.Tk, z.max_kv, kv_lens == nullptr);
+    if (st != HYD_OK) return st;
+    return !workspace || (uintptr_t)workspace % kAlign != 0 || bytes < need ? HYD_ERR_WORKSPACE : HYD_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -186,8 +309,7 @@ size_t hyd_cross_attn_workspace_bytes(int total_q, int total_kv, int num_seqs, i
                                       int head_dim, hyd_dtype dt, int is_bwd) {
     const Sizes z{total_q, total_kv, num_seqs, max_seqlen_q, max_seqlen_kv, hq, hkv, head_dim, dt};
     if (check_sizes(z) != HYD_OK) return 0;
-    (void)is_bwd;
-    return fwd_layout(z).total;
+    return is_bwd ? bwd_layout(z).total : fwd_layout(z).total;
 }
 
 hyd_status hyd_cross_attn_fwd(const void* q, const void* k, const void* v, const int32_t* cu_q, const int32_t* cu_kv, const int32_t* kv_lens,
@@ -198,17 +320,39 @@ hyd_status hyd_cross_attn_fwd(const void* q, const void* k, const void* v, const
     hyd_status st = check_sizes(z);
     if (st != HYD_OK) return st;
     if (dt != HYD_BF16) return HYD_ERR_DTYPE;
-    if (total_q == 0 || num_seqs == 0) return HYD_OK;
-    if (max_seqlen_q == 0) return HYD_ERR_SHAPE;
-    if (!cu_q || !cu_kv || !q || !o || !lse || (total_kv > 0 && (!k || !v))) return HYD_ERR_NULL;
-    if ((st = check_lengths(cu_q_host, num_seqs, total_q, max_seqlen_q, true)) != HYD_OK) return st;
-    if ((st = check_lengths(cu_kv_host, num_seqs, total_kv, max_seqlen_kv, kv_lens == nullptr)) != HYD_OK) return st;
-    if (!workspace || (uintptr_t)workspace % kAlign != 0 || workspace_bytes < fwd_layout(z).need) return HYD_ERR_WORKSPACE;
+    if (total_q == 0) return HYD_OK;
+    bool nothing = false;
+    st = check_call(z, cu_q, cu_kv, kv_lens, cu_q_host, cu_kv_host, q && o && lse && (total_kv == 0 || (k && v)), workspace, workspace_bytes,
+                    fwd_layout(z).need, &nothing);
+    if (st != HYD_OK || nothing) return st;
     int cus = 0;
     if ((st = cross_device(&cus)) != HYD_OK) return st;
     const CrossShape c = shape_of(z, cu_q, cu_kv, kv_lens);
     const auto launch = head_dim == 64 ? launch_fwd<64> : launch_fwd<128>;
     launch(z, c, q, k, v, softmax_scale, o, lse, static_cast<char*>(workspace), workspace_bytes, cus, static_cast<hipStream_t>(hip_stream));
+    return hipGetLastError() == hipSuccess ? HYD_OK : HYD_ERR_LAUNCH;
+}
+
+hyd_status hyd_cross_attn_bwd(const void* q, const void* k, const void* v, const void* o, const float* lse, const void* d_o,
+                              const int32_t* cu_q, const int32_t* cu_kv, const int32_t* kv_lens, int num_seqs, const int32_t* cu_q_host,
+                              const int32_t* cu_kv_host, int total_q, int total_kv, int max_seqlen_q, int max_seqlen_kv, int hq, int hkv,
+                              int head_dim, float softmax_scale, hyd_dtype dt, void* dq, void* dk, void* dv, void* workspace,
+                              size_t workspace_bytes, void* hip_stream) {
+    const Sizes z{total_q, total_kv, num_seqs, max_seqlen_q, max_seqlen_kv, hq, hkv, head_dim, dt};
+    hyd_status st = check_sizes(z);
+    if (st != HYD_OK) return st;
+    if (dt != HYD_BF16) return HYD_ERR_DTYPE;
+    bool nothing = false;
+    st = check_call(z, cu_q, cu_kv, kv_lens, cu_q_host, cu_kv_host,
+                    (total_q == 0 || (q && o && lse && d_o && dq)) && (total_kv == 0 || (k && v && dk && dv)), workspace, workspace_bytes,
+                    bwd_layout(z).need, &nothing);
+    if (st != HYD_OK || nothing) return st;
+    int cus = 0;
+    if ((st = cross_device(&cus)) != HYD_OK) return st;
+    const CrossShape c = shape_of(z, cu_q, cu_kv, kv_lens);
+    const BwdArgs a{q, k, v, o, lse, d_o, dq, dk, dv};
+    const auto launch = head_dim == 64 ? launch_bwd<64> : launch_bwd<128>;
+    launch(z, c, a, softmax_scale, static_cast<char*>(workspace), workspace_bytes, cus, static_cast<hipStream_t>(hip_stream));
     return hipGetLastError() == hipSuccess ? HYD_OK : HYD_ERR_LAUNCH;
 }
 

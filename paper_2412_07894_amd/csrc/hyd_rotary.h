@@ -11,7 +11,7 @@
 // a unit being C pairs (two loads of C elements, 16 bytes each where alignment allows) or 2 C elements behind the
 // turned part, which are only copied.  The first units are requested before the table is formed.
 #pragma once
-#include "hyd_device.h"
+#include "hyd_find.h"
 
 namespace hyd {
 
@@ -28,28 +28,6 @@ struct RotParams {
     float mag;
     int inverse, in_place;                // in_place: nothing is copied
 };
-
-// The sequence that holds packed row t, by a whole wave: s and its first row and end; false if t lies in none.  64 probes at a time.
-__device__ __forceinline__ bool rot_find(const int32_t* __restrict__ cu, int nseq, int t, int& s, int& first, int& end) {
-    const int lane = threadIdx.x & 63;
-    int lo = 0, n = nseq + 1;             // the last index i in [lo, lo + n) with cu[i] <= t, if there is one
-    while (true) {
-        const int step = (n + 63) / 64, i = lo + lane * step;
-        const int c = lane * step < n ? cu[i] : 0x7fffffff;
-        const int k = __popcll(__ballot(c <= t));
-        if (k == 0) return false;
-        lo += (k - 1) * step;
-        n = min(step, n - (k - 1) * step);
-        if (n == 1) {
-            first = __shfl(c, k - 1, 64);
-            break;
-        }
-    }
-    if (lo >= nseq) return false;
-    s = lo;
-    end = cu[lo + 1];
-    return true;
-}
 
 template <typename E, int C> struct RotVec { E v[C]; };
 template <int C, typename E>
@@ -115,7 +93,7 @@ __global__ void __launch_bounds__(kRotThreads) hyd_rotary_kernel(RotParams p) {
         bool in = false;
         for (int r = 0; r < nt; ++r) {
             const int t = t0 + r;
-            if (!in || t >= end) in = rot_find(p.cu, p.nseq, t, s, first, end);
+            if (!in || t >= end) in = find_sequence(p.cu, p.nseq, t, s, first, end);
             if (tid == 0) pos[r] = in ? (long long)(t - first) + (p.starts ? p.starts[s] : 0) : kNone;
         }
     }

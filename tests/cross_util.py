@@ -4,10 +4,10 @@ bf16 forward.  A rounding to bf16 is off by at most u = 2^-8 of the value.  P is
 u sum_j P_ij |V_j| + u |O|, and what the scores' fp32 sums (d terms, each 2^-24 of sum |q k|) and the exponentials add.
 LSE: no rounding to bf16 enters; the scores' error and a few units of 2^-24 of its own size.
 
-bf16 backward.  P and dS are rounded to fp16 (h = 2^-11 of the value, 2^-25 absolutely below its normal range, with dO scaled to a
-largest value in [1, 2)), results to bf16:
-  dV: h sum P |dO|;  dQ, dK: h sum |dS| |K| and h sum |dS| |Q|, and as dS = P (dP - D) is formed in fp32 from a P that is rounded
-  already in dK's case, once more; and from the scores' error e_s, which moves every P by e_s of itself.
+bf16 backward, given O and LSE.  P and dS are rounded to fp16 (h = 2^-11 of the value, 2^-25 absolutely below its normal range; dO is
+scaled to a largest value in [1, 2), so there 2^-25 counts in units of that), results to bf16; in dK, dS is formed from a P that is
+rounded already.  The scores' error e moves every P by e of itself, the fp32 sums of dP every dS by P times theirs; fp16 copies of
+elements below 2^-14 keep 2^-25.
 fp32: products and sums in fp32, d + n terms."""
 import numpy as np
 import torch
@@ -101,3 +101,43 @@ def check_fwd(c, o, lse, what=""):
     if c.dtype == "bf16" and norm > 0 and ref_o.size > 4096:
         # two roundings of 2^-8 / sqrt(3) * 0.74 each (errors uniform in a step, mantissas log-uniform), and a quarter more
         assert np.sqrt((err_o ** 2).sum()) / norm < 1.25 * np.sqrt(2) * 0.74 * 2.0 ** -8 / np.sqrt(3), what
+
+
+def check_bwd(c, o, lse, dq, dk, dv, what=""):
+    """Gradients against the reference's backward of the same O and LSE."""
+    q, k, v = c.cpu()
+    do, o, lse = (np.nan_to_num(np64(x), nan=0.0) for x in (c.do, o, lse))
+    ref = co.bwd(q, k, v, o, lse, do, c.cq, c.ck, c.scale, c.kv_lens)
+    tol = [np.zeros(x.shape) for x in (q, k, v)]
+    bf = c.dtype == "bf16"
+    u, h, tiny, e, group = U[c.dtype], 2.0 ** -11 if bf else 0.0, 2.0 ** -25 if bf else 0.0, score_error(c), c.hq // c.hkv
+    big = np.abs(do[c.q_rows]).max(initial=0.0)
+    for s, n in enumerate(c.n):
+        rows, keys = slice(int(c.cq[s]), int(c.cq[s + 1])), slice(int(c.ck[s]), int(c.ck[s]) + n)
+        if n == 0 or c.lq[s] == 0:
+            continue
+        acc = (max(n, c.lq[s] * group) + c.d) * 2.0 ** -24
+        for hd in range(c.hq):
+            g = hd // group
+            Q, K, V, dO, O = q[rows, hd], k[keys, g], v[keys, g], do[rows, hd], o[rows, hd]
+            L = lse[hd, rows, None]
+            P = np.exp(c.scale * (Q @ K.T) - L)
+            dP, D = dO @ V.T, (dO * O).sum(1, keepdims=True)
+            dS = np.abs(P * (dP - D))
+            e2 = 2 * e + 2.0 ** -21 * (1 + np.abs(L)) + acc
+            # dP: its sums, fp16 copies of V and of the scaled dO that are below the normal range, D's sum
+            edp = 2 * c.d * 2.0 ** -24 * (np.abs(dO) @ np.abs(V).T + np.abs(dO * O).sum(1, keepdims=True)) + tiny * (np.abs(dO).sum(1, keepdims=True) + big * np.abs(V).sum(1)[None])
+            tol[0][rows, hd] += abs(c.scale) * (((h + e2) * dS + P * edp + 2 * tiny * big) @ (np.abs(K) + tiny))
+            tol[1][keys, g] += abs(c.scale) * (((2 * h + e2) * dS + P * edp + tiny * np.abs(dP - D) + 4 * tiny * big).T @ (np.abs(Q) + tiny))
+            tol[2][keys, g] += ((h + e2) * P + tiny).T @ np.abs(dO) + P.sum(0)[:, None] * tiny * big
+    for name, got, r, t, on in zip(("dq", "dk", "dv"), (dq, dk, dv), ref, tol, (c.q_rows, c.kv_rows, c.kv_rows)):
+        got, r, t = np64(got)[on], r[on], t[on]
+        t = t + u * (1 + u) * np.abs(r) + 1e-30
+        assert np.all(np.isfinite(got)), f"{what} {name} is not finite"
+        err = np.abs(got - r)
+        assert np.all(err <= t), f"{what} {name}: off by {np.max(err / t):.2f} of the bound"
+        norm = np.sqrt((r ** 2).sum())
+        if bf and norm > 0 and r.size > 4096:
+            # one rounding of 2^-8 / sqrt(3) * 0.74, those to fp16 are an eighth of it; a quarter more
+            rel = np.sqrt((err ** 2).sum()) / norm
+            assert rel < 1.25 * 0.74 * 2.0 ** -8 / np.sqrt(3), f"{what} {name}: rel {rel:.3e}"

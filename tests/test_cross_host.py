@@ -58,7 +58,28 @@ def test_forward_host_lengths(lib, cq, ck, code):
     assert fwd(lib, **{"cqh" if cq else "ckh": p}) == code
 
 
+def bwd(lib, **kw):
+    a = dict(q=P, k=P, v=P, o=P, lse=P, do=P, cq=P, ck=P, kl=None, nseq=2, cqh=None, ckh=None, Tq=100, Tk=300, mq=60, mk=200, hq=4, hkv=2, d=128,
+             scale=0.1, dt=0, dq=P, dk=P, dv=P, ws=P, wb=1 << 32)
+    a.update(kw)
+    return lib.hyd_cross_attn_bwd(a["q"], a["k"], a["v"], a["o"], a["lse"], a["do"], a["cq"], a["ck"], a["kl"], a["nseq"], a["cqh"], a["ckh"],
+                                  a["Tq"], a["Tk"], a["mq"], a["mk"], a["hq"], a["hkv"], a["d"], a["scale"], a["dt"], a["dq"], a["dk"], a["dv"],
+                                  a["ws"], a["wb"], None)
+
+
+@pytest.mark.parametrize("kw,code", COMMON + [(dict([(n, None)]), NULL) for n in ("o", "lse", "do", "dq", "dk", "dv")])
+def test_backward_refusals(lib, kw, code):
+    assert bwd(lib, **kw) == code
+
+
+@pytest.mark.parametrize("cq,ck,code", SEQ)
+def test_backward_host_lengths(lib, cq, ck, code):
+    keep, p = host(cq or ck)
+    assert bwd(lib, **{"cqh" if cq else "ckh": p}) == code
+
+
 def test_nothing_to_do(lib):
+    assert bwd(lib, Tq=0, mq=0, Tk=0, mk=0) == OK and bwd(lib, Tq=0, mq=0, Tk=0, mk=0, nseq=0, ws=None) == OK
     assert fwd(lib, Tq=0, mq=0) == OK and fwd(lib, Tq=0, mq=0, nseq=0) == OK
     assert fwd(lib, Tq=0, mq=0, q=None, o=None, ws=None, wb=0) == OK
 
