@@ -174,11 +174,11 @@ __device__ __forceinline__ void store_packed_rows(AtFn at, int rows, const f32x1
 constexpr int kCrossMaxParts = 64, kCrossJoinThreads = 256;
 struct CrossJoin {
     const float* part_o; const float* part_lse;      // [parts][Tq][Hq][d], [parts][Hq][Tq]
-    uint16_t* o; float* lse;
+    void* o; float* lse;
     const int32_t* cu_q;
     int nseq, Tq, hq, parts;
 };
-template <int D>
+template <int D, bool kF32>
 __global__ void __launch_bounds__(kCrossJoinThreads) hyd_cross_join_kernel(CrossJoin p) {
     constexpr int kLanes = D / 4, kRows = kCrossJoinThreads / kLanes;
     const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / kLanes;
@@ -200,8 +200,9 @@ __global__ void __launch_bounds__(kCrossJoinThreads) hyd_cross_join_kernel(Cross
         sum += *reinterpret_cast<const f32x4*>(p.part_o + i * plane + row * D + 4 * c) * w;
     }
     const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);      // (a NaN stays one)
-    const u32x2 w = {pack_bf16(sum[0] * inv, sum[1] * inv), pack_bf16(sum[2] * inv, sum[3] * inv)};
-    *reinterpret_cast<u32x2*>(p.o + row * D + 4 * c) = w;
+    sum *= inv;
+    if (kF32) *reinterpret_cast<f32x4*>(static_cast<float*>(p.o) + row * D + 4 * c) = sum;
+    else *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.o) + row * D + 4 * c) = u32x2{pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3])};
     if (c == 0) p.lse[(int64_t)h * p.Tq + t] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
 }
 

@@ -4,6 +4,7 @@
 #include <mutex>
 
 #include "hyd_cross_bwd.h"
+#include "hyd_cross_fp32.h"
 #include "hyd_cross_fwd.h"
 #include "hyd_host.h"
 
@@ -46,6 +47,8 @@ hyd_status check_lengths(const int32_t* cu, int nseq, int T, int most, bool boun
     return HYD_OK;
 }
 
+int tile_q(hyd_dtype dt) { return dt == HYD_BF16 ? kFwdBM : kF32BM; }
+int tile_kv(hyd_dtype dt) { return dt == HYD_BF16 ? kKwBN : kF32KvBN; }
 long long tiles(long long rows, int tile) { return (rows + tile - 1) / tile; }
 // tiles of nseq sequences with `total` rows, none longer than `most`, at most
 long long most_tiles(long long total, long long most, int nseq, int tile) {
@@ -59,13 +62,13 @@ constexpr size_t kPartRoomRows = 65536;   // rows (tokens times query heads, tim
 FwdLayout fwd_layout(const Sizes& z) {
     FwdLayout w;
     const int G = z.hq / z.hkv;
-    w.max_items = most_tiles((long long)z.Tq * G, (long long)z.max_q * G, z.nseq, kFwdBM);
+    w.max_items = most_tiles((long long)z.Tq * G, (long long)z.max_q * G, z.nseq, tile_q(z.dt));
     size_t at = 0;
     w.hdr = at;   at += align_up(sizeof(int) * kHdrTotal);
     w.items = at; at += align_up(16 * (size_t)(w.max_items > 0 ? w.max_items : 1));
     w.need = at;
     const size_t rows = (size_t)z.Tq * z.hq, most = kCrossMaxParts * rows < kPartRoomRows ? kCrossMaxParts * rows : kPartRoomRows;
-    w.total = at + (z.dt == HYD_BF16 ? align_up(most * (size_t)z.d * 4) + align_up(most * 4) : 0);
+    w.total = at + align_up(most * (size_t)z.d * 4) + align_up(most * 4);
     return w;
 }
 
@@ -82,8 +85,8 @@ struct BwdLayout { size_t q_hdr, q_items, kv_hdr, kv_items, stat[4], q16, do16, 
 BwdLayout bwd_layout(const Sizes& z) {
     BwdLayout w;
     const int G = z.hq / z.hkv;
-    w.n_q = most_tiles((long long)z.Tq * G, (long long)z.max_q * G, z.nseq, kDqBM);
-    w.n_kv = most_tiles(z.Tk, z.max_kv, z.nseq, kKwBN);
+    w.n_q = most_tiles((long long)z.Tq * G, (long long)z.max_q * G, z.nseq, tile_q(z.dt));
+    w.n_kv = most_tiles(z.Tk, z.max_kv, z.nseq, tile_kv(z.dt));
     const size_t q_elems = (size_t)z.Tq * z.hq * z.d, kv_elems = (size_t)z.Tk * z.hkv * z.d;
     const auto records = [](long long n) { return align_up(16 * (size_t)(n > kBwdItems ? n : kBwdItems)); };      // (parts: kBwdItems records at most)
     size_t at = 0;
@@ -91,6 +94,11 @@ BwdLayout bwd_layout(const Sizes& z) {
     w.q_items = at;  at += records(w.n_q);
     w.kv_hdr = at;   at += align_up(sizeof(int) * kHdrTotal);
     w.kv_items = at; at += records(w.n_kv);
+    if (z.dt == HYD_FP32) {
+        w.stat[0] = at; at += align_up(sizeof(float) * (size_t)z.Tq * z.hq);
+        w.need = w.total = at;
+        return w;
+    }
     for (size_t& s : w.stat) { s = at; at += align_up(sizeof(float) * (size_t)z.Tq * z.hq); }
     w.q16 = at;      at += align_up(2 * q_elems);
     w.do16 = at;     at += align_up(2 * q_elems);
@@ -125,7 +133,9 @@ template <int D>
 bool prep_kernels() {
     return allow_lds(hyd_cross_fwd_bf16_kernel<D, false>, kFwdLds) && allow_lds(hyd_cross_fwd_bf16_kernel<D, true>, kFwdLds) &&
            allow_lds(hyd_cross_few_bf16_kernel<D>, kFewLds) && allow_lds(hyd_cross_dq_bf16_kernel<D>, kDqLds) &&
-           allow_lds(hyd_bwd_dkdv_wide_bf16_kernel<D, CrossBwdParams>, kKwLds);
+           allow_lds(hyd_bwd_dkdv_wide_bf16_kernel<D, CrossBwdParams>, kKwLds) && allow_lds(hyd_cross_fwd_fp32_kernel<D, false>, f32_lds<D>()) &&
+           allow_lds(hyd_cross_fwd_fp32_kernel<D, true>, f32_lds<D>()) && allow_lds(hyd_cross_dq_fp32_kernel<D>, f32_lds<D>()) &&
+           allow_lds(hyd_cross_dkdv_fp32_kernel<D>, f32_lds<D>());
 }
 hyd_status cross_device(int* cus) {
     int dev = 0;
@@ -149,10 +159,10 @@ CrossShape shape_of(const Sizes& z, const int32_t* cu_q, const int32_t* cu_kv, c
 }
 
 template <int D>
-void launch_join(const CrossJoin& j, hipStream_t st) {
+void launch_join(const CrossJoin& j, bool f32, hipStream_t st) {
     constexpr int kRows = kCrossJoinThreads / (D / 4);
     KernelTimer kt("cross_join", st);
-    hipLaunchKernelGGL(hyd_cross_join_kernel<D>, dim3((unsigned)tiles((long long)j.Tq * j.hq, kRows)), dim3(kCrossJoinThreads), 0, st, j);
+    hipLaunchKernelGGL((f32 ? hyd_cross_join_kernel<D, true> : hyd_cross_join_kernel<D, false>), dim3((unsigned)tiles((long long)j.Tq * j.hq, kRows)), dim3(kCrossJoinThreads), 0, st, j);
 }
 
 template <int D>
@@ -161,14 +171,14 @@ void launch_fwd(const Sizes& z, const CrossShape& c, const void* q, const void* 
     const FwdLayout w = fwd_layout(z);
     CrossJoin j;
     j.part_o = reinterpret_cast<float*>(ws + w.need);
-    j.o = static_cast<uint16_t*>(o); j.lse = lse; j.cu_q = c.cu_q; j.nseq = z.nseq; j.Tq = z.Tq; j.hq = z.hq; j.parts = 1;
+    j.o = o; j.lse = lse; j.cu_q = c.cu_q; j.nseq = z.nseq; j.Tq = z.Tq; j.hq = z.hq; j.parts = 1;
     const long long rows = (long long)z.max_q * c.G;
     const auto part_lse = [&](int parts) { return reinterpret_cast<float*>(ws + w.need + align_up((size_t)parts * z.Tq * z.hq * z.d * 4)); };
-    if (rows <= kFewRows) {
+    if (z.dt == HYD_BF16 && rows <= kFewRows) {
         CrossFewParams p;
         p.c = c;
         p.q = static_cast<const uint16_t*>(q); p.k = static_cast<const uint16_t*>(k); p.v = static_cast<const uint16_t*>(v);
-        p.o = j.o; p.lse = lse; p.scale_log2 = scale * kLog2eHost;
+        p.o = static_cast<uint16_t*>(o); p.lse = lse; p.scale_log2 = scale * kLog2eHost;
         const long long items = (long long)z.nseq * z.hkv;
         constexpr int kTurn = kFewWaves * kFewKeys;
         long long want = items >= kCus ? tiles(8 * kCus, items) : kCus / items;
@@ -182,37 +192,48 @@ void launch_fwd(const Sizes& z, const CrossShape& c, const void* q, const void* 
         KernelTimer kt("cross_few", st);
         hipLaunchKernelGGL(hyd_cross_few_bf16_kernel<D>, dim3((unsigned)(items * p.parts)), dim3(kFewThreads), kFewLds, st, p);
     } else {
-        CrossFwdParams p;
-        p.c = c;
-        p.q = static_cast<const uint16_t*>(q); p.k = static_cast<const uint16_t*>(k); p.v = static_cast<const uint16_t*>(v);
-        p.o = j.o; p.lse = lse; p.scale_log2 = scale * kLog2eHost;
-        p.hdr = reinterpret_cast<int*>(ws + w.hdr); p.cursors = reinterpret_cast<int*>(ws + w.hdr) + kHdrCursor; p.items = reinterpret_cast<int*>(ws + w.items);
-        p.tiles = (int)tiles(rows, kFwdBM);
-        const long long own = (long long)z.nseq * p.tiles * z.hkv;
+        // items of whole tiles: own ones where they all fit on the chip, with the keys in parts where they do not fill it, else from a list
+        const int tile = tile_q(z.dt), key_tile = z.dt == HYD_BF16 ? kFwdBN : kF32Tile;
+        const long long per_seq = tiles(rows, tile), own = (long long)z.nseq * per_seq * z.hkv;
         const bool self = own <= kCus;
         long long want = 1;
         if (self) {
-            want = kCus / own;
-            const long long most = tiles(z.max_kv, 4 * kFwdBN);
-            if (want > most) want = most;
+            const long long most = tiles(z.max_kv, 4 * key_tile);
+            want = kCus / own < most ? kCus / own : most;
             if (want > kCrossMaxParts) want = kCrossMaxParts;
         }
-        j.parts = p.parts = want > 1 ? parts_in_room(w, z, ws_bytes, (int)want) : 1;
-        p.part_o = const_cast<float*>(j.part_o); p.part_lse = part_lse(j.parts);
-        long long grid = self ? own * p.parts : w.max_items * z.hkv;
+        j.parts = want > 1 ? parts_in_room(w, z, ws_bytes, (int)want) : 1;
+        long long grid = self ? own * j.parts : w.max_items * z.hkv;
         if (!self && grid > cus) grid = cus;
-        p.hm = head_map_kv(z.hkv, (int)grid);
+        int* hdr = reinterpret_cast<int*>(ws + w.hdr); int* items = reinterpret_cast<int*>(ws + w.items);
         if (!self) {
-            const CrossList l{reinterpret_cast<int*>(ws + w.hdr), reinterpret_cast<int*>(ws + w.items), kFwdBM, 1, (int)w.max_items, false};
+            const CrossList l{hdr, items, tile, 1, (int)w.max_items, false};
             KernelTimer kt("cross_list", st);
             hipLaunchKernelGGL(hyd_cross_list_kernel, dim3(1), dim3(kPreludeThreads), kCrossListLds, st, c, l);
         }
+        const auto common = [&](auto& p) {
+            p.c = c; p.hdr = hdr; p.cursors = hdr + kHdrCursor; p.items = items; p.hm = head_map_kv(z.hkv, (int)grid);
+            p.parts = j.parts; p.tiles = (int)per_seq; p.part_o = const_cast<float*>(j.part_o); p.part_lse = part_lse(j.parts);
+        };
         KernelTimer kt("cross_fwd", st);
-        hipLaunchKernelGGL((self ? hyd_cross_fwd_bf16_kernel<D, true> : hyd_cross_fwd_bf16_kernel<D, false>), dim3((unsigned)grid), dim3(kFwdThreads), kFwdLds, st, p);
+        if (z.dt == HYD_BF16) {
+            CrossFwdParams p;
+            common(p);
+            p.q = static_cast<const uint16_t*>(q); p.k = static_cast<const uint16_t*>(k); p.v = static_cast<const uint16_t*>(v);
+            p.o = static_cast<uint16_t*>(o); p.lse = lse; p.scale_log2 = scale * kLog2eHost;
+            hipLaunchKernelGGL((self ? hyd_cross_fwd_bf16_kernel<D, true> : hyd_cross_fwd_bf16_kernel<D, false>), dim3((unsigned)grid), dim3(kFwdThreads), kFwdLds, st, p);
+        } else {
+            CrossF32Params p;
+            memset(&p, 0, sizeof(p));
+            common(p);
+            p.q = static_cast<const float*>(q); p.k = static_cast<const float*>(k); p.v = static_cast<const float*>(v);
+            p.o_out = static_cast<float*>(o); p.lse_out = lse; p.scale = scale;
+            hipLaunchKernelGGL((self ? hyd_cross_fwd_fp32_kernel<D, true> : hyd_cross_fwd_fp32_kernel<D, false>), dim3((unsigned)grid), dim3(64 * kF32Waves), f32_lds<D>(), st, p);
+        }
     }
     if (j.parts > 1) {
         j.part_lse = part_lse(j.parts);
-        launch_join<D>(j, st);
+        launch_join<D>(j, z.dt == HYD_FP32, st);
     }
 }
 
@@ -288,6 +309,42 @@ void launch_bwd(const Sizes& z, const CrossShape& c, const BwdArgs& a, float sca
             launch_sum<D>(CrossSum{part + (size_t)which * parts_kv * kv_rows * D, static_cast<uint16_t*>(which ? a.dv : a.dk), c.cu_kv, c.kv_lens, z.nseq, z.Tk, z.hkv, parts_kv}, st);
 }
 
+template <int D>
+void launch_bwd_f32(const Sizes& z, const CrossShape& c, const BwdArgs& a, float scale, char* ws, size_t, int cus, hipStream_t st) {
+    const BwdLayout w = bwd_layout(z);
+    int* hdr[2] = {reinterpret_cast<int*>(ws + w.q_hdr), reinterpret_cast<int*>(ws + w.kv_hdr)};
+    int* items[2] = {reinterpret_cast<int*>(ws + w.q_items), reinterpret_cast<int*>(ws + w.kv_items)};
+    {
+        CrossF32Begin b;
+        b.c = c; b.dk = static_cast<float*>(a.dk); b.dv = static_cast<float*>(a.dv); b.d = D;
+        b.lists[0] = CrossList{hdr[0], items[0], kF32BM, 1, (int)w.n_q, false};
+        b.lists[1] = CrossList{hdr[1], items[1], kF32KvBN, 1, (int)w.n_kv, true};
+        const int n_zero = !c.kv_lens ? 0 : (z.nseq < kCus ? z.nseq : kCus);
+        KernelTimer kt("cross_begin", st);
+        hipLaunchKernelGGL(hyd_cross_begin_fp32_kernel, dim3(2 + n_zero), dim3(kPreludeThreads), kCrossListLds, st, b);
+    }
+    CrossF32Params p;
+    memset(&p, 0, sizeof(p));
+    p.c = c; p.scale = scale; p.parts = 1;
+    p.q = static_cast<const float*>(a.q); p.k = static_cast<const float*>(a.k); p.v = static_cast<const float*>(a.v);
+    p.o = static_cast<const float*>(a.o); p.d_o = static_cast<const float*>(a.d_o); p.lse_in = a.lse;
+    p.dq = static_cast<float*>(a.dq); p.dk = static_cast<float*>(a.dk); p.dv = static_cast<float*>(a.dv);
+    p.D = reinterpret_cast<float*>(ws + w.stat[0]);
+    const auto take = [&](int list, long long work) {
+        const int grid = (int)(work < 1 ? 1 : (work < cus ? work : cus));
+        p.hdr = hdr[list]; p.cursors = hdr[list] + kHdrCursor; p.items = items[list]; p.hm = head_map_kv(z.hkv, grid);
+        return grid;
+    };
+    {
+        const int grid = take(0, w.n_q * z.hkv);
+        KernelTimer kt("cross_dq", st);
+        hipLaunchKernelGGL(hyd_cross_dq_fp32_kernel<D>, dim3(grid), dim3(64 * kF32Waves), f32_lds<D>(), st, p);
+    }
+    const int grid = take(1, w.n_kv * z.hkv);
+    KernelTimer kt("cross_dkdv", st);
+    hipLaunchKernelGGL(hyd_cross_dkdv_fp32_kernel<D>, dim3(grid), dim3(64 * kF32KvWaves), f32_lds<D>(), st, p);
+}
+
 // What both directions check before any HIP call; HYD_OK with *nothing set: there is nothing to do.
 hyd_status check_call(const Sizes& z, const int32_t* cu_q, const int32_t* cu_kv, const int32_t* kv_lens, const int32_t* cu_q_host,
                       const int32_t* cu_kv_host, bool pointers, const void* workspace, size_t bytes, size_t need, bool* nothing) {
@@ -319,7 +376,6 @@ hyd_status hyd_cross_attn_fwd(const void* q, const void* k, const void* v, const
     const Sizes z{total_q, total_kv, num_seqs, max_seqlen_q, max_seqlen_kv, hq, hkv, head_dim, dt};
     hyd_status st = check_sizes(z);
     if (st != HYD_OK) return st;
-    if (dt != HYD_BF16) return HYD_ERR_DTYPE;
     if (total_q == 0) return HYD_OK;
     bool nothing = false;
     st = check_call(z, cu_q, cu_kv, kv_lens, cu_q_host, cu_kv_host, q && o && lse && (total_kv == 0 || (k && v)), workspace, workspace_bytes,
@@ -341,7 +397,6 @@ hyd_status hyd_cross_attn_bwd(const void* q, const void* k, const void* v, const
     const Sizes z{total_q, total_kv, num_seqs, max_seqlen_q, max_seqlen_kv, hq, hkv, head_dim, dt};
     hyd_status st = check_sizes(z);
     if (st != HYD_OK) return st;
-    if (dt != HYD_BF16) return HYD_ERR_DTYPE;
     bool nothing = false;
     st = check_call(z, cu_q, cu_kv, kv_lens, cu_q_host, cu_kv_host,
                     (total_q == 0 || (q && o && lse && d_o && dq)) && (total_kv == 0 || (k && v && dk && dv)), workspace, workspace_bytes,
@@ -351,7 +406,7 @@ hyd_status hyd_cross_attn_bwd(const void* q, const void* k, const void* v, const
     if ((st = cross_device(&cus)) != HYD_OK) return st;
     const CrossShape c = shape_of(z, cu_q, cu_kv, kv_lens);
     const BwdArgs a{q, k, v, o, lse, d_o, dq, dk, dv};
-    const auto launch = head_dim == 64 ? launch_bwd<64> : launch_bwd<128>;
+    const auto launch = dt == HYD_FP32 ? (head_dim == 64 ? launch_bwd_f32<64> : launch_bwd_f32<128>) : (head_dim == 64 ? launch_bwd<64> : launch_bwd<128>);
     launch(z, c, a, softmax_scale, static_cast<char*>(workspace), workspace_bytes, cus, static_cast<hipStream_t>(hip_stream));
     return hipGetLastError() == hipSuccess ? HYD_OK : HYD_ERR_LAUNCH;
 }

@@ -141,3 +141,38 @@ def test_graph_stream_and_repeats():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, ref)), rep
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (6, 2), (20, 20), (40, 1)])
+def test_fp32_lengths(hq, hkv, d):
+    lq = [1, 0, 31, 33, 64, 200, 257, 1, 5, 300, 17]
+    kv = [1, 50, 63, 64, 65, 0, 129, 300, 31, 1, 32]
+    both(Case(lq, kv, hq, hkv, d, "fp32", seed=hq + d), f"{hq}/{hkv}")
+
+
+@pytest.mark.parametrize("scale", [-0.1, 0.0, 0.5])
+def test_fp32_scales_padding_and_outside_rows(scale):
+    c = Case([3, 140, 300, 7, 0], [130, 400, 70, 64, 9], 4, 2, 128, "fp32", kv_lens=[100, 350, 0, 1, -4], scale=scale, seed=5, front=13, back=9)
+    o, lse = c.fwd()
+    dq, dk, dv = torch.full_like(c.q, 7.0), torch.full_like(c.k, 7.0), torch.full_like(c.v, 7.0)
+    c.bwd(o, lse, dq=dq, dk=dk, dv=dv)
+    check_bwd(c, o, lse, dq, dk, dv)
+    for x, on in ((dq, c.q_rows), (dk, c.kv_rows), (dv, c.kv_rows)):
+        assert torch.all(x[torch.from_numpy(~on).cuda()] == 7.0)
+
+
+def test_fp32_list_with_many_sequences_and_missing_sides():
+    rng = np.random.default_rng(8)
+    lq, kv = rng.integers(0, 90, 300), rng.integers(0, 120, 300)
+    lq[5], kv[5], kv[9] = 900, 600, 1100
+    both(Case(lq, kv, 6, 3, 64, "fp32", seed=9))
+    c = Case([0, 0], [30, 300], 2, 2, 64, "fp32", seed=10)
+    c.max_q = 0
+    dk, dv = torch.full_like(c.k, 7.0), torch.full_like(c.v, 7.0)
+    c.bwd(c.q, torch.zeros((2, 0), device="cuda"), dk=dk, dv=dv)
+    assert torch.all(dk == 0) and torch.all(dv == 0)
+    c = Case([20, 300], [0, 0], 2, 2, 64, "fp32", seed=10)
+    o, lse = c.fwd()
+    dq, _, _ = c.bwd(o, lse, dq=torch.full_like(c.q, 7.0))
+    assert torch.all(o == 0) and torch.all(dq == 0)

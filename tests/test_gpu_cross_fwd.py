@@ -138,3 +138,33 @@ def test_offsets_past_32_bits(lq):
     small = lambda x: torch.cat([x[s * rows:s * rows + 300] for s in range(n)])
     o2, lse2 = binding.cross_attn_fwd(q, small(k), small(v), cq, torch.arange(n + 1, dtype=torch.int32, device="cuda") * 300, lq, 300, 0.1)
     assert torch.equal(o, o2) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (6, 2), (20, 20), (40, 1)])
+def test_fp32_lengths(hq, hkv, d):
+    lq = [1, 0, 31, 33, 64, 200, 257, 1, 5, 300, 17]
+    kv = [1, 50, 63, 64, 65, 0, 129, 300, 31, 1, 32]
+    c = Case(lq, kv, hq, hkv, d, "fp32", seed=hq + d)
+    check_fwd(c, *c.fwd(), what=f"{hq}/{hkv}")
+
+
+@pytest.mark.parametrize("lq", [[1, 2, 1, 1], [40, 100, 7, 260]])
+@pytest.mark.parametrize("scale", [-0.1, 0.0, 1.0])
+def test_fp32_scales_padding_and_parts(lq, scale):
+    c = Case(lq, [130, 2500, 70, 64], 4, 2, 128, "fp32", kv_lens=[100, 2400, 0, 900], scale=scale, seed=5, front=13, back=9)
+    o, lse = torch.full_like(c.q, 7.0), torch.full((4, c.Tq), 7.0, device="cuda")
+    c.fwd(out=o, lse=lse)
+    check_fwd(c, o, lse)
+    off = torch.from_numpy(~c.q_rows).cuda()
+    assert torch.all(o[off] == 7.0) and torch.all(lse[:, off] == 7.0)
+    ws = torch.empty(64 * 1024, dtype=torch.uint8, device="cuda")         # too little for parts
+    check_fwd(c, *c.fwd(workspace=ws))
+
+
+def test_fp32_list_with_many_sequences():
+    rng = np.random.default_rng(8)
+    lq, kv = rng.integers(0, 90, 300), rng.integers(0, 120, 300)
+    lq[5], kv[5], kv[9] = 900, 600, 1100
+    c = Case(lq, kv, 6, 3, 64, "fp32", seed=9)
+    check_fwd(c, *c.fwd())
