@@ -135,24 +135,20 @@ def _stream_ptr(stream):
     return ctypes.c_void_p(s.cuda_stream)
 
 
-class _on:
-    """The device of a call's tensors, made the current one where it is not."""
-    def __init__(self, device):
-        if device.type != "cuda":
-            raise ValueError(f"tensors must be on a GPU, got {device}")
-        self.other = torch.cuda.device(device) if device.index != torch.cuda.current_device() else None
-
-    def __enter__(self):
-        if self.other is not None:
-            self.other.__enter__()
-
-    def __exit__(self, *exc):
-        if self.other is not None:
-            self.other.__exit__(*exc)
-
-
-def _stream_of(device, stream):
-    return (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream
+def _on_device(device, call, args, stream):
+    """call(*args, stream) with the device of the call's tensors as the current one, on `stream` or else that device's current one.
+    (Small calls take as long as the host does: the stream's handle and the device are asked for without an object around them.)"""
+    if device.type != "cuda":
+        raise ValueError(f"tensors must be on a GPU, got {device}")
+    index = device.index
+    handle = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+    if index == torch._C._cuda_getDevice():
+        code = call(*args, handle)
+    else:
+        with torch.cuda.device(index):
+            code = call(*args, handle)
+    if code != 0:
+        raise HydError(code, status_string(code))
 
 
 def varlen_attn_fwd(q, k, v, cu_seqlens, max_seqlen, softmax_scale, cu_seqlens_host=None,
@@ -322,7 +318,7 @@ def _like(name, t, shape, dtype, device):
     """t as it is, checked; made if None."""
     if t is None:
         return torch.empty(shape, dtype=dtype, device=device)
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device or not t.is_contiguous():
+    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {tuple(shape)} tensor of {dtype} on {device}, got {tuple(t.shape)} {t.dtype} {t.device}")
     return t
 
@@ -333,7 +329,8 @@ def _cross_sizes(q, k, v, cu_q, cu_kv, max_seqlen_q, max_seqlen_kv, workspace, i
         raise ValueError(f"q and k must be [rows, heads, d], got {tuple(q.shape)} and {tuple(k.shape)}")
     (Tq, hq, d), (Tk, hkv, _), dev = q.shape, k.shape, q.device
     dt = _dtype_code(q)
-    _like("q", q, (Tq, hq, d), q.dtype, dev)
+    if not q.is_contiguous():
+        raise ValueError(f"q must be contiguous, got strides {q.stride()}")
     _like("k", k, (Tk, hkv, d), q.dtype, dev)
     _like("v", v, (Tk, hkv, d), q.dtype, dev)
     nseq = cu_q.numel() - 1
@@ -363,11 +360,10 @@ def cross_attn_fwd(q, k, v, cu_q, cu_kv, max_seqlen_q, max_seqlen_kv, softmax_sc
     lse = _like("lse", lse, (hq, Tq), torch.float32, dev)
     kq, hp_q = _host_lens("cu_q_host", cu_q_host, nseq)
     kk, hp_k = _host_lens("cu_kv_host", cu_kv_host, nseq)
-    with _on(dev):
-        _check(load().hyd_cross_attn_fwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), _int32("cu_q", cu_q, nseq + 1, dev),
-                                         _int32("cu_kv", cu_kv, nseq + 1, dev), _int32("kv_lens", kv_lens, nseq, dev), nseq, hp_q, hp_k,
-                                         Tq, Tk, int(max_seqlen_q), int(max_seqlen_kv), hq, hkv, d, float(softmax_scale), dt,
-                                         o.data_ptr(), lse.data_ptr(), ws.data_ptr(), ws.numel(), _stream_of(dev, stream)))
+    _on_device(dev, load().hyd_cross_attn_fwd,
+               (q.data_ptr(), k.data_ptr(), v.data_ptr(), _int32("cu_q", cu_q, nseq + 1, dev), _int32("cu_kv", cu_kv, nseq + 1, dev),
+                _int32("kv_lens", kv_lens, nseq, dev), nseq, hp_q, hp_k, Tq, Tk, int(max_seqlen_q), int(max_seqlen_kv), hq, hkv, d,
+                float(softmax_scale), dt, o.data_ptr(), lse.data_ptr(), ws.data_ptr(), ws.numel()), stream)
     return o, lse
 
 
@@ -385,12 +381,11 @@ def cross_attn_bwd(q, k, v, o, lse, d_o, cu_q, cu_kv, max_seqlen_q, max_seqlen_k
     dv = _like("dv", dv, v.shape, v.dtype, dev)
     kq, hp_q = _host_lens("cu_q_host", cu_q_host, nseq)
     kk, hp_k = _host_lens("cu_kv_host", cu_kv_host, nseq)
-    with _on(dev):
-        _check(load().hyd_cross_attn_bwd(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), d_o.data_ptr(),
-                                         _int32("cu_q", cu_q, nseq + 1, dev), _int32("cu_kv", cu_kv, nseq + 1, dev),
-                                         _int32("kv_lens", kv_lens, nseq, dev), nseq, hp_q, hp_k, Tq, Tk, int(max_seqlen_q),
-                                         int(max_seqlen_kv), hq, hkv, d, float(softmax_scale), dt, dq.data_ptr(), dk.data_ptr(),
-                                         dv.data_ptr(), ws.data_ptr(), ws.numel(), _stream_of(dev, stream)))
+    _on_device(dev, load().hyd_cross_attn_bwd,
+               (q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), d_o.data_ptr(), _int32("cu_q", cu_q, nseq + 1, dev),
+                _int32("cu_kv", cu_kv, nseq + 1, dev), _int32("kv_lens", kv_lens, nseq, dev), nseq, hp_q, hp_k, Tq, Tk, int(max_seqlen_q),
+                int(max_seqlen_kv), hq, hkv, d, float(softmax_scale), dt, dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), ws.data_ptr(),
+                ws.numel()), stream)
     return dq, dk, dv
 
 
@@ -406,20 +401,23 @@ def rope_frequencies(rot_dim, base=10000.0, scaling="plain", factor=1.0, origina
 
 
 def _rope_tensor(name, x, out, T, d, dt, device):
-    """Checks a tensor of rope_rotate and its output (made if None): [T, heads, d], the heads of a token contiguous."""
-    if x.dim() != 3 or x.shape[0] != T or x.shape[2] != d or x.dtype != dt or x.device != device:
-        raise ValueError(f"{name} must be [{T}, heads, {d}] in {dt} on {device}, got {tuple(x.shape)} {x.dtype} {x.device}")
+    """Checks a tensor of rope_rotate and its output (made if None), [T, heads, d] with the heads of a token contiguous: (output,
+    heads, the tensor's token stride, the output's)."""
+    shape = x.shape
+    if len(shape) != 3 or shape[0] != T or shape[2] != d or x.dtype != dt or x.device != device:
+        raise ValueError(f"{name} must be [{T}, heads, {d}] in {dt} on {device}, got {tuple(shape)} {x.dtype} {x.device}")
     if out is None:
-        out = torch.empty(x.shape, dtype=dt, device=device)
-    if out.shape != x.shape or out.dtype != dt or out.device != device:
+        out = torch.empty(shape, dtype=dt, device=device)
+    elif out.shape != shape or out.dtype != dt or out.device != device:
         raise ValueError(f"the output of {name} must be like it, got {tuple(out.shape)} {out.dtype} {out.device}")
-    row = x.shape[1] * d
-    strides = []
+    heads = shape[1]
+    token = []
     for t in (x, out):
-        if T and ((d > 1 and t.stride(2) != 1) or (t.shape[1] > 1 and t.stride(1) != d) or (T > 1 and t.stride(0) < row)):
-            raise ValueError(f"{name}: the heads of a token must be contiguous, got strides {t.stride()}")
-        strides.append(t.stride(0) if T > 1 else row)
-    return out, strides[0], strides[1]
+        st = t.stride()
+        if T and ((d > 1 and st[2] != 1) or (heads > 1 and st[1] != d) or (T > 1 and st[0] < heads * d)):
+            raise ValueError(f"{name}: the heads of a token must be contiguous, got strides {st}")
+        token.append(st[0] if T > 1 else heads * d)
+    return out, heads, token[0], token[1]
 
 
 def _int32(name, t, n, device):
@@ -452,17 +450,15 @@ def rope_rotate(q, freqs, k=None, cu_seqlens=None, starts=None, positions=None, 
     nseq = 0 if cu_seqlens is None else cu_seqlens.numel() - 1
     if nseq < 0:
         raise ValueError("cu_seqlens must have num_seqs + 1 elements")
-    out, qs, qos = _rope_tensor("q", q, out, T, d, q.dtype, dev)
-    hk, ks, kos = 0, 0, 0
+    out, hq, qs, qos = _rope_tensor("q", q, out, T, d, q.dtype, dev)
+    kp, kop, hk, ks, kos = None, None, 0, 0, 0
     if k is not None:
-        k_out, ks, kos = _rope_tensor("k", k, k_out, T, d, q.dtype, dev)
-        hk = k.shape[1]
-    with _on(dev):
-        _check(load().hyd_rope_rotate(q.data_ptr(), hq, qs, out.data_ptr(), qos, k.data_ptr() if hk else None, hk, ks,
-                                      k_out.data_ptr() if hk else None, kos, _int32("cu_seqlens", cu_seqlens, nseq + 1, dev),
-                                      _int32("starts", starts, nseq, dev), nseq, _int32("positions", positions, T, dev), T, d,
-                                      freqs.data_ptr(), 2 * freqs.numel(), ROPE_LAYOUTS[layout], float(magnitude),
-                                      int(bool(inverse)), dt, _stream_of(dev, stream)))
+        k_out, hk, ks, kos = _rope_tensor("k", k, k_out, T, d, q.dtype, dev)
+        kp, kop = k.data_ptr(), k_out.data_ptr()
+    _on_device(dev, load().hyd_rope_rotate,
+               (q.data_ptr(), hq, qs, out.data_ptr(), qos, kp, hk, ks, kop, kos, _int32("cu_seqlens", cu_seqlens, nseq + 1, dev),
+                _int32("starts", starts, nseq, dev), nseq, _int32("positions", positions, T, dev), T, d, freqs.data_ptr(),
+                2 * freqs.numel(), ROPE_LAYOUTS[layout], float(magnitude), int(bool(inverse)), dt), stream)
     return out if k is None else (out, k_out)
 
 

@@ -5,6 +5,7 @@
 
 #include "hyd_cross_bwd.h"
 #include "hyd_cross_fp32.h"
+#include "hyd_cross_keys.h"
 #include "hyd_cross_fwd.h"
 #include "hyd_host.h"
 
@@ -133,6 +134,7 @@ template <int D>
 bool prep_kernels() {
     return allow_lds(hyd_cross_fwd_bf16_kernel<D, false>, kFwdLds) && allow_lds(hyd_cross_fwd_bf16_kernel<D, true>, kFwdLds) &&
            allow_lds(hyd_cross_few_bf16_kernel<D>, kFewLds) && allow_lds(hyd_cross_dq_bf16_kernel<D>, kDqLds) &&
+           allow_lds(hyd_cross_bwd_keys_bf16_kernel<D>, kKeysLds) &&
            allow_lds(hyd_bwd_dkdv_wide_bf16_kernel<D, CrossBwdParams>, kKwLds) && allow_lds(hyd_cross_fwd_fp32_kernel<D, false>, f32_lds<D>()) &&
            allow_lds(hyd_cross_fwd_fp32_kernel<D, true>, f32_lds<D>()) && allow_lds(hyd_cross_dq_fp32_kernel<D>, f32_lds<D>()) &&
            allow_lds(hyd_cross_dkdv_fp32_kernel<D>, f32_lds<D>());
@@ -240,7 +242,7 @@ void launch_fwd(const Sizes& z, const CrossShape& c, const void* q, const void* 
 template <int D>
 void launch_sum(const CrossSum& x, hipStream_t st) {
     KernelTimer kt("cross_sum", st);
-    hipLaunchKernelGGL(hyd_cross_sum_kernel<D>, dim3((unsigned)x.T), dim3(kCrossSumThreads), 0, st, x);
+    hipLaunchKernelGGL(hyd_cross_sum_kernel<D>, dim3((unsigned)x.T, x.out[1] ? 2 : 1), dim3(kCrossSumThreads), 0, st, x);
 }
 
 struct BwdArgs { const void *q, *k, *v, *o; const float* lse; const void* d_o; void *dq, *dk, *dv; };
@@ -257,6 +259,23 @@ void launch_bwd(const Sizes& z, const CrossShape& c, const BwdArgs& a, float sca
     const size_t room = ws_bytes - w.need, q_rows = (size_t)z.Tq * z.hq, kv_rows = (size_t)z.Tk * z.hkv;
     const int parts_q = bwd_parts(w.n_q * z.hkv, kCus, tiles(z.max_kv, kDqBN), 8, q_rows, kDqPartRows, (size_t)D * 4, room);
     const int parts_kv = bwd_parts(w.n_kv * z.hkv, kBwdItems, tiles((long long)z.max_q * G, kKwBM), 8, kv_rows, kKvPartRows, (size_t)D * 8, room);
+    if (z.max_kv <= kKeysMax && z.max_kv > 0) {
+        CrossKeysParams p;
+        p.c = c;
+        p.q = static_cast<const uint16_t*>(a.q); p.k = static_cast<const uint16_t*>(a.k); p.v = static_cast<const uint16_t*>(a.v);
+        p.o = static_cast<const uint16_t*>(a.o); p.d_o = static_cast<const uint16_t*>(a.d_o); p.lse = a.lse;
+        p.dq = static_cast<uint16_t*>(a.dq); p.dk = static_cast<uint16_t*>(a.dk); p.dv = static_cast<uint16_t*>(a.dv);
+        const long long items = (long long)z.nseq * z.hkv;
+        p.parts = bwd_parts(items, kBwdItems, tiles((long long)z.max_q * G, kKeysBM), 4, kv_rows, kKvPartRows, (size_t)D * 8, room);
+        p.part = part; p.scale = scale; p.scale_log2 = scale * kLog2eHost;
+        {
+            KernelTimer kt("cross_bwd_keys", st);
+            hipLaunchKernelGGL(hyd_cross_bwd_keys_bf16_kernel<D>, dim3((unsigned)(items * p.parts)), dim3(kKeysThreads), kKeysLds, st, p);
+        }
+        if (p.parts > 1)
+            launch_sum<D>(CrossSum{part, {p.dk, p.dv}, c.cu_kv, c.kv_lens, z.nseq, z.Tk, z.hkv, p.parts}, st);
+        return;
+    }
     int* q_hdr = reinterpret_cast<int*>(ws + w.q_hdr); int* kv_hdr = reinterpret_cast<int*>(ws + w.kv_hdr);
     int* q_items = reinterpret_cast<int*>(ws + w.q_items); int* kv_items = reinterpret_cast<int*>(ws + w.kv_items);
     const long long work_q = w.n_q * z.hkv * parts_q, work_kv = w.n_kv * z.hkv * parts_kv;
@@ -288,7 +307,7 @@ void launch_bwd(const Sizes& z, const CrossShape& c, const BwdArgs& a, float sca
         KernelTimer kt("cross_dq", st);
         hipLaunchKernelGGL(hyd_cross_dq_bf16_kernel<D>, dim3(grid), dim3(kDqThreads), kDqLds, st, p, l);
     }
-    if (parts_q > 1) launch_sum<D>(CrossSum{part, static_cast<uint16_t*>(a.dq), c.cu_q, nullptr, z.nseq, z.Tq, z.hq, parts_q}, st);
+    if (parts_q > 1) launch_sum<D>(CrossSum{part, {static_cast<uint16_t*>(a.dq), nullptr}, c.cu_q, nullptr, z.nseq, z.Tq, z.hq, parts_q}, st);
     if (z.Tk == 0) return;
     {
         CrossBwdParams p;
@@ -305,8 +324,7 @@ void launch_bwd(const Sizes& z, const CrossShape& c, const BwdArgs& a, float sca
         hipLaunchKernelGGL((hyd_bwd_dkdv_wide_bf16_kernel<D, CrossBwdParams>), dim3(grid), dim3(kKwThreads), kKwLds, st, p, l);
     }
     if (parts_kv > 1)
-        for (int which = 0; which < 2; ++which)
-            launch_sum<D>(CrossSum{part + (size_t)which * parts_kv * kv_rows * D, static_cast<uint16_t*>(which ? a.dv : a.dk), c.cu_kv, c.kv_lens, z.nseq, z.Tk, z.hkv, parts_kv}, st);
+        launch_sum<D>(CrossSum{part, {static_cast<uint16_t*>(a.dk), static_cast<uint16_t*>(a.dv)}, c.cu_kv, c.kv_lens, z.nseq, z.Tk, z.hkv, parts_kv}, st);
 }
 
 template <int D>

@@ -350,7 +350,7 @@ __global__ void __launch_bounds__(kDqThreads, 1) hyd_cross_dq_bf16_kernel(CrossD
 // ---------------------------------------------------------------------------------------------
 constexpr int kCrossSumThreads = 256;
 struct CrossSum {
-    const float* part; uint16_t* out;
+    const float* part; uint16_t* out[2];          // [outputs][parts] planes
     const int32_t* cu; const int32_t* lens;       // lens: NULL, or valid rows of a sequence
     int nseq, T, heads, parts;
 };
@@ -364,10 +364,10 @@ __global__ void __launch_bounds__(kCrossSumThreads) hyd_cross_sum_kernel(CrossSu
     }
     const int64_t row = (int64_t)p.heads * D, plane = (int64_t)p.T * row;
     for (int i = 4 * threadIdx.x; i < p.heads * D; i += 4 * kCrossSumThreads) {
-        const float* src = p.part + t * row + i;
+        const float* src = p.part + blockIdx.y * (int64_t)p.parts * plane + t * row + i;
         f32x4 sum = *reinterpret_cast<const f32x4*>(src);
         for (int x = 1; x < p.parts; ++x) sum += *reinterpret_cast<const f32x4*>(src + x * plane);
-        *reinterpret_cast<u32x2*>(p.out + t * row + i) = u32x2{pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3])};
+        *reinterpret_cast<u32x2*>(p.out[blockIdx.y] + t * row + i) = u32x2{pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3])};
     }
 }
 

@@ -26,6 +26,34 @@ def test_lengths(hq, hkv, d):
 
 
 @pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (2, 2), (6, 2), (8, 1), (20, 20), (10, 5), (40, 1), (16, 8)])
+def test_few_keys(hq, hkv, d):
+    """At most 128 keys: the form that streams the rows once."""
+    lq = [1, 0, 31, 33, 64, 200, 257, 1, 5, 300, 17, 700]
+    kv = [1, 50, 63, 64, 65, 0, 128, 127, 31, 96, 32, 77]
+    both(Case(lq, kv, hq, hkv, d, seed=hq + d), f"{hq}/{hkv}")
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_few_keys_padded_in_parts_and_scaled(d):
+    for scale, size in ((None, 1.0), (-0.2, 1e-6), (0.0, 1e4)):
+        c = Case([3, 2000, 0, 7, 1500], [130, 400, 70, 64, 9], 4, 2, d, kv_lens=[100, 128, 900, 0, -4], scale=scale, seed=5, front=13, back=9)
+        c.do *= size
+        assert c.max_kv <= 128
+        o, lse = c.fwd()
+        outs = []
+        for ws in (None, torch.empty(64 << 20, dtype=torch.uint8, device="cuda").fill_(255)):
+            dq, dk, dv = torch.full_like(c.q, 7.0), torch.full_like(c.k, 7.0), torch.full_like(c.v, 7.0)
+            c.bwd(o, lse, dq=dq, dk=dk, dv=dv, workspace=ws)
+            check_bwd(c, o, lse, dq, dk, dv)
+            for x, on in ((dq, c.q_rows), (dk, c.kv_rows), (dv, c.kv_rows)):
+                off = torch.from_numpy(~on).cuda()
+                assert off.sum() == 22 and torch.all(x[off] == 7.0)
+            outs.append((dq, dk, dv))
+        assert all(torch.equal(a, b) for a, b in zip(*outs))
+
+
+@pytest.mark.parametrize("d", [64, 128])
 def test_padded_and_outside_rows(d):
     """Padding and rows of no sequence hold nan and are not read; dK and dV are 0 in the padding, outputs of rows of no sequence
     stay as they were."""
