@@ -134,7 +134,7 @@ template <int D>
 bool prep_kernels() {
     return allow_lds(hyd_cross_fwd_bf16_kernel<D, false>, kFwdLds) && allow_lds(hyd_cross_fwd_bf16_kernel<D, true>, kFwdLds) &&
            allow_lds(hyd_cross_few_bf16_kernel<D>, kFewLds) && allow_lds(hyd_cross_dq_bf16_kernel<D>, kDqLds) &&
-           allow_lds(hyd_cross_bwd_keys_bf16_kernel<D>, kKeysLds) &&
+           allow_lds(hyd_cross_bwd_keys_bf16_kernel<D>, KeysForm<D>::kLds) &&
            allow_lds(hyd_bwd_dkdv_wide_bf16_kernel<D, CrossBwdParams>, kKwLds) && allow_lds(hyd_cross_fwd_fp32_kernel<D, false>, f32_lds<D>()) &&
            allow_lds(hyd_cross_fwd_fp32_kernel<D, true>, f32_lds<D>()) && allow_lds(hyd_cross_dq_fp32_kernel<D>, f32_lds<D>()) &&
            allow_lds(hyd_cross_dkdv_fp32_kernel<D>, f32_lds<D>());
@@ -266,11 +266,11 @@ void launch_bwd(const Sizes& z, const CrossShape& c, const BwdArgs& a, float sca
         p.o = static_cast<const uint16_t*>(a.o); p.d_o = static_cast<const uint16_t*>(a.d_o); p.lse = a.lse;
         p.dq = static_cast<uint16_t*>(a.dq); p.dk = static_cast<uint16_t*>(a.dk); p.dv = static_cast<uint16_t*>(a.dv);
         const long long items = (long long)z.nseq * z.hkv;
-        p.parts = bwd_parts(items, kBwdItems, tiles((long long)z.max_q * G, kKeysBM), 4, kv_rows, kKvPartRows, (size_t)D * 8, room);
+        p.parts = bwd_parts(items, kBwdItems, tiles((long long)z.max_q * G, KeysForm<D>::kBM), 4, kv_rows, kKvPartRows, (size_t)D * 8, room);
         p.part = part; p.scale = scale; p.scale_log2 = scale * kLog2eHost;
         {
             KernelTimer kt("cross_bwd_keys", st);
-            hipLaunchKernelGGL(hyd_cross_bwd_keys_bf16_kernel<D>, dim3((unsigned)(items * p.parts)), dim3(kKeysThreads), kKeysLds, st, p);
+            hipLaunchKernelGGL(hyd_cross_bwd_keys_bf16_kernel<D>, dim3((unsigned)(items * p.parts)), dim3(kKeysThreads), KeysForm<D>::kLds, st, p);
         }
         if (p.parts > 1)
             launch_sum<D>(CrossSum{part, {p.dk, p.dv}, c.cu_kv, c.kv_lens, z.nseq, z.Tk, z.hkv, p.parts}, st);

@@ -1,34 +1,42 @@
 // Cross attention, backward in bf16 where a sequence has few keys (at most kKeysMax), as when an image or sound model looks at a
 // prompt: all three gradients in one pass over the rows.
 //
-// The general backward goes over Q and dO three times and writes copies of both (hyd_cross_bwd.h), which is what a call with few keys
-// takes: 9 units of HBM traffic (a unit: Q once) where 4 have to be, Q, dO and O read and dQ written.  Here the keys of a (sequence, KV
-// head) stay in registers, 32 for each of four waves, and tiles of 64 packed rows stream past them:
-//     S = Q K^T, P = exp2(S scale - LSE2), dP = dO V^T - D, dS = P dP        (one key per lane, rows in the slots)
-//     dV^T += dO^T P, dK^T += Q^T dS                                        (the wave's keys)
-//     dQ^T = K^T dS^T                  (dS of all keys meets in LDS; a wave forms 32 columns of the head, for d = 64 of 32 rows)
-// D = rowsum(dO * O) and LSE2 of a tile are formed one tile ahead.
+// The general backward goes over Q and dO three times and writes copies of both (hyd_cross_bwd.h): 9 units of HBM traffic (a unit:
+// Q once) where 4 have to be, Q, dO and O read and dQ written.  Here the keys of a (sequence, KV head) stay in registers, 32 for each of
+// four pairs of waves, and tiles of 64 packed rows stream past them (one key per lane, rows in the slots):
+//     first waves:   S = Q K^T, P = exp2(S scale - LSE2), handed over through LDS, dV^T += dO^T P
+//     second waves:  dP = dO V^T - D, dS = P dP, dK^T += Q^T dS
+//     then all:      dQ^T = K^T dS^T, a block of 32 rows and 32 columns of the head each    (dS of all keys meets in LDS)
+// D = rowsum(dO * O) and LSE2 of a tile are formed one tile ahead.  The two waves of a pair share a SIMD, so that one's vector work
+// runs under the other's products.
 //
 // Arithmetic.  P and dS enter the second products as two bf16 numbers, the rounded value and the rest, 16 bits together, so that
 // every product runs on the bf16 MFMA with Q, K, dO as they are: no scaling of dO, no copies, and no range but bf16's own.
 //
-// Bound by HBM for 64 keys and more rows.  Each tile has two barriers: the first opens the tile (and says that the stage before the
-// last has been read by all), the second publishes dS.
+// A tile has three barriers: the first opens it (and says that the stage before the last has been read by all), the second hands P
+// over, the third publishes dS.
 #pragma once
 #include "hyd_cross_bwd.h"
 
 namespace hyd {
 
-constexpr int kKeysMax = 128, kKeysWaves = 4, kKeysThreads = 64 * kKeysWaves, kKeysBM = 64, kKeysStages = 3;
-constexpr int kKeysTileBytes = kKeysBM * kRowBytes, kKeysStageBytes = 2 * kKeysTileBytes;         // Q, dO
-// dS: [hi, lo][key][64 rows] bf16; the 32-byte quarter of rows 16 q .. of a key lies at q ^ ds_swz(key), so that the transposing reads
-// (four keys, 32 rows) meet no bank twice
-constexpr int kKeysDsOff = kKeysStages * kKeysStageBytes, kKeysDsRow = kKeysBM * 2, kKeysDsBytes = kKeysMax * kKeysDsRow;
-constexpr int kKeysStatOff = kKeysDsOff + 2 * kKeysDsBytes;                                        // [parity][LSE2, D][64]
-constexpr int kKeysLds = kKeysStatOff + 4 * kKeysBM * 4;
+constexpr int kKeysMax = 128, kKeysPairs = 4, kKeysWaves = 2 * kKeysPairs, kKeysThreads = 64 * kKeysWaves;
+// Tiles.  A row of a tile in LDS is 256 bytes: a row of d = 128, or rows r and r + 64 of d = 64, whose tiles have 128 rows then.
+// (What a tile takes is mostly waiting for the step before, so tiles are as large as registers and LDS allow.)
+template <int D> struct KeysForm {
+    static constexpr int kBM = D == 64 ? 128 : 64, kBlocks = kBM / 32, kStages = D == 64 ? 2 : 3;
+    static constexpr int kTileBytes = 64 * kRowBytes, kStageBytes = 2 * kTileBytes;                // Q, dO
+    // dS: [hi, lo][key][row] bf16; the 32 bytes of rows 16 q .. of a key lie at q ^ swz(key), so that the transposing reads (four keys, 32
+    // rows) meet no bank twice.  Before, the bytes of a pair's keys hold its P: [row block][4 slots][lane] floats.
+    static constexpr int kDsOff = kStages * kStageBytes, kDsRow = kBM * 2, kDsBytes = kKeysMax * kDsRow;
+    static constexpr int kStatOff = kDsOff + 2 * kDsBytes;                                         // [parity][LSE2, D][row]
+    static constexpr int kLds = kStatOff + 4 * kBM * 4;
+    static_assert(kKeysMax * kRowBytes <= kStageBytes && kKeysMax * kRowBytes <= 2 * kDsBytes, "K and V rows while an item begins");
+    static_assert(32 * kDsRow == kBlocks / 2 * 64 * 16 * 4, "P of half the row blocks in the place of half of dS");
+    __device__ __forceinline__ static int swz(int key) { return D == 64 ? ((key & 3) << 1) | ((key >> 2) & 1) : (((key >> 1) & 1) << 1) | ((key >> 2) & 1); }
+    __device__ __forceinline__ static constexpr int p_off(int rb) { return rb / (kBlocks / 2) * kDsBytes + rb % (kBlocks / 2) * 4096; }
+};
 constexpr int kKeysOutRow = 80;           // bytes of a row of 32 dQ columns in LDS
-static_assert(kKeysMax * kRowBytes <= kKeysStageBytes && kKeysMax * kRowBytes <= 2 * kKeysDsBytes, "K and V rows while an item begins");
-__device__ __forceinline__ int ds_swz(int key) { return (((key >> 1) & 1) << 1) | ((key >> 2) & 1); }
 
 struct CrossKeysParams {
     CrossShape c;
@@ -40,6 +48,7 @@ struct CrossKeysParams {
 };
 
 // LDS stores beside direct-to-LDS loads in flight, in assembly for the reason given at lds_issue_row
+__device__ __forceinline__ void lds_store(uint32_t addr, u32x4 v, int off) { asm volatile("ds_write_b128 %0, %1 offset:%2" : : "v"(addr), "v"(v), "i"(off) : "memory"); }
 __device__ __forceinline__ void lds_store(uint32_t addr, u32x2 v) { asm volatile("ds_write_b64 %0, %1" : : "v"(addr), "v"(v) : "memory"); }
 __device__ __forceinline__ void lds_store(uint32_t addr, float v) { asm volatile("ds_write_b32 %0, %1" : : "v"(addr), "v"(v) : "memory"); }
 // two floats as pairs of bf16: rounded values, and what they leave
@@ -48,20 +57,33 @@ __device__ __forceinline__ void split_bf16(float a, float b, uint32_t& hi, uint3
     lo = pack_bf16(a - bf16_lo(hi), b - bf16_hi(hi));
 }
 
+// A wave's direct-to-LDS loads of a tile: N of them, kStep rows apart.  (D keeps the two kernels' instances apart: the compiler's host
+// pass, which does not know the instruction, drops whoever calls an instance for the second time.)
+template <int D, int kStep, int N>
+__device__ __forceinline__ void dma_at(const __amdgpu_buffer_rsrc_t& rs, char* lds, const uint32_t (&voff)[N]) {
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void_c*)(lds + kStep * j * kRowBytes), 16, voff[j], 0, 0, 0);
+}
+
+struct KeysRows { int t0, rem, rows; };       // a tile: token of its first row, that row's head in the group, rows
+
 template <int D>
 __global__ void __launch_bounds__(kKeysThreads, 1) hyd_cross_bwd_keys_bf16_kernel(CrossKeysParams p) {
-    extern __shared__ __attribute__((aligned(16))) char smem[];
-    constexpr int kRowB = D * 2, NK = D / 16, NDB = D / 32, NV = D / 32;
-    constexpr int kDma = 2 * 64 * kRowBytes / 1024 / kKeysWaves;              // loads of a tile by each wave
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    using F = KeysForm<D>;
+    constexpr int kRowB = D * 2, NK = D / 16, NDB = D / 32, kBM = F::kBM, kBlocks = F::kBlocks;
+    constexpr int kPerRow = kKeysThreads / kBM, NV = kRowB / 16 / kPerRow;     // threads that form a row's statistics, 16-byte pieces of each
+    constexpr int kDma = F::kStageBytes / 1024 / kKeysWaves;                   // loads of a tile by each wave
     const int tid = threadIdx.x, lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), pair = wave & (kKeysPairs - 1);
     const int l32 = lane & 31, half = lane >> 5, lane16 = lane & 15;
     const int g = blockIdx.x % p.c.hkv, part = (blockIdx.x / p.c.hkv) % p.parts, seq = blockIdx.x / p.c.hkv / p.parts;
     const CrossSeq x = cross_seq(p.c, seq);
     const int G = p.c.G, n = min(x.n, kKeysMax), rows_all = x.lq * G;
     const int64_t q_stride = (int64_t)p.c.hq * D, kv_stride = (int64_t)p.c.hkv * D;
     const uint32_t kv_stride_b = (uint32_t)kv_stride * 2, q_stride_b = (uint32_t)q_stride * 2;
-    const int n_all = (rows_all + kKeysBM - 1) / kKeysBM, per_part = (n_all + p.parts - 1) / p.parts;
+    const int n_all = (rows_all + kBM - 1) / kBM, per_part = (n_all + p.parts - 1) / p.parts;
     const int t_lo = min(part * per_part, n_all), t_hi = min(t_lo + per_part, n_all);
     const int64_t kv_at = (int64_t)x.k0 * kv_stride + (int64_t)g * D;
     CrossRows cr;
@@ -73,48 +95,84 @@ __global__ void __launch_bounds__(kKeysThreads, 1) hyd_cross_bwd_keys_bf16_kerne
             *reinterpret_cast<u32x4*>(p.dv + at) = u32x4{0u, 0u, 0u, 0u};
         }
     if (n == 0) {                                         // no keys: dQ = 0
-        for (int i = t_lo * kKeysBM * (D / 8) + tid; i < min(t_hi * kKeysBM, rows_all) * (D / 8); i += kKeysThreads) {
+        for (int i = t_lo * kBM * (D / 8) + tid; i < min(t_hi * kBM, rows_all) * (D / 8); i += kKeysThreads) {
             const int r = i / (D / 8), token = r / G;
             *reinterpret_cast<u32x4*>(p.dq + (x.q0 + token) * q_stride + (int64_t)(g * G + r - token * G) * D + 8 * (i % (D / 8))) = u32x4{0u, 0u, 0u, 0u};
         }
         return;
     }
-    FragAddr fa;
-    fa.init(lane, smem);
+    // Fragment addresses (see FragAddr): those of the contraction steps of a row fragment differ in bits 5-7 only, those of the column
+    // blocks of a column fragment in bits 6-7 and its second row group in bit 5 besides 8 rows.
+    uint32_t row_frag, col_frag;
+    {
+        FragAddr fa;
+        fa.init(lane, smem);
+        row_frag = fa.row[0];
+        col_frag = fa.col[0];
+    }
+    const auto issue_column = [](LdsQueue& q, ColFrag& f, uint32_t at, int c, int off) {
+        lds_issue_col(q, f, at ^ (uint32_t)(c << 6), (at + 8 * kRowBytes) ^ (uint32_t)(c << 6 | 32), off);
+    };
     const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_char*)smem;
     const float scale_log2 = fmaxf(fabsf(p.scale_log2), 1e-30f);
     const uint32_t sign_flip = p.scale_log2 < 0.f ? 0x80008000u : 0u;
 
-    // ---- row tiles
-    struct Rows { int t0, rem, rows; };                   // token of the first row, its head in the group, rows of the tile
-    const auto tile_rows = [&](int t) -> Rows {
-        const int r = t * kKeysBM, token = r / G;
-        return Rows{x.q0 + token, r - token * G, min(rows_all - r, kKeysBM)};
+    // ---- row tiles.  Where G divides a tile's rows holds whole tokens, and where its rows lie in it is the same for every tile; else
+    // both are found by division, tile by tile.
+    const bool whole = kBM % G == 0;
+    const int per_tile = whole ? kBM / G : 0;         // tokens of a tile
+    const auto tile_rows = [&](int t) -> KeysRows {
+        const int r = t * kBM, rows = min(rows_all - r, kBM);
+        if (whole) return KeysRows{x.q0 + t * per_tile, 0, rows};
+        const int token = r / G;
+        return KeysRows{x.q0 + token, r - token * G, rows};
     };
-    const auto tile_rsrc = [&](const uint16_t* base, const Rows& w) {
-        return make_rsrc(base + (int64_t)w.t0 * q_stride + (int64_t)g * G * D, (uint32_t)((w.rem + w.rows - 1) / G) * q_stride_b + (uint32_t)G * kRowB);
+    const auto tile_rsrc = [&](const uint16_t* base, const KeysRows& w, bool on) {
+        // (bounded by the sequence's last row: those behind it are cut here, or by their offset where tokens are not whole)
+        return make_rsrc(base + (int64_t)w.t0 * q_stride + (int64_t)g * G * D, on ? (uint32_t)(min(x.q0 + x.lq - w.t0, kBM + 1) - 1) * q_stride_b + (uint32_t)G * kRowB : 0u);
     };
+    constexpr int kRowLoads = kDma / 2;                   // loads of a tensor's tile by each wave
+    uint32_t voff[kRowLoads], soff;                       // this lane's rows: of the tile loads, and of the statistics
+    const auto find_rows = [&](int rem, int rows) {
+        int ln = lane, token, head;
+        asm volatile("" : "+v"(ln));
+        const int row = 4 * wave + (ln >> 4), chunk = (ln & 15) ^ swz(row);
+#pragma unroll
+        for (int j = 0; j < kRowLoads; ++j) {
+            const int r = row + 4 * kKeysWaves * j + (D == kHeadDim ? 0 : 64 * (chunk / (D / 8)));
+            cr.split(rem + r, token, head);
+            voff[j] = r < rows ? (uint32_t)token * q_stride_b + (uint32_t)(head * kRowB + (chunk % (D / 8) << 4)) : kDmaOutOfRange;
+        }
+        cr.split(rem + tid / kPerRow, token, head);
+        soff = tid / kPerRow < rows ? (uint32_t)token * q_stride_b + (uint32_t)(head * kRowB + tid % kPerRow * (kRowB / kPerRow)) : kDmaOutOfRange;
+    };
+    if (whole) find_rows(0, kBM);
+    // Tiles behind the last one are asked for too, of a resource without bytes: with the loads under a condition, the compiler does not
+    // know how many are under way, and waits for all of them where it needs the statistics, whose loads are older.
     auto load_tile = [&](int t, int stage) {
-        const Rows w = tile_rows(t);
-        dma_packed_rows<kKeysWaves, D>(tile_rsrc(p.q, w), smem + stage * kKeysStageBytes, [](int) { return 0; }, 1, cr, w.rem, w.rows, q_stride_b, wave, lane);
-        dma_packed_rows<kKeysWaves, D>(tile_rsrc(p.d_o, w), smem + stage * kKeysStageBytes + kKeysTileBytes, [](int) { return 0; }, 1, cr, w.rem, w.rows, q_stride_b, wave, lane);
+        const KeysRows w = tile_rows(min(t, t_hi - 1));
+        if (!whole) find_rows(w.rem, w.rows);
+        const __amdgpu_buffer_rsrc_t rq = tile_rsrc(p.q, w, t < t_hi), rd = tile_rsrc(p.d_o, w, t < t_hi);
+        char* d = smem + stage * F::kStageBytes + 4 * wave * kRowBytes;
+        dma_at<D, 4 * kKeysWaves>(rq, d, voff);
+        dma_at<D, 4 * kKeysWaves>(rd, d + F::kTileBytes, voff);
     };
-    // statistics: four threads to a row
     u32x4 so[NV], sd[NV];
     float sl = 0.f;
     auto load_stats = [&](int t) {
-        const Rows w = tile_rows(t);
-        const __amdgpu_buffer_rsrc_t ro = tile_rsrc(p.o, w), rd = tile_rsrc(p.d_o, w);
-        const int r = tid >> 2;
-        int token, head;
-        cr.split(w.rem + r, token, head);
-        const uint32_t at = r < w.rows ? (uint32_t)token * q_stride_b + (uint32_t)(head * kRowB + (tid & 3) * (kRowB / 4)) : kDmaOutOfRange;
+        const KeysRows w = tile_rows(min(t, t_hi - 1));
+        if (!whole) find_rows(w.rem, w.rows);
+        const __amdgpu_buffer_rsrc_t ro = tile_rsrc(p.o, w, t < t_hi), rd = tile_rsrc(p.d_o, w, t < t_hi);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            so[i] = __builtin_amdgcn_raw_buffer_load_b128(ro, at, 16 * i, 0);
-            sd[i] = __builtin_amdgcn_raw_buffer_load_b128(rd, at, 16 * i, 0);
+            so[i] = __builtin_amdgcn_raw_buffer_load_b128(ro, soff, 16 * i, 0);
+            sd[i] = __builtin_amdgcn_raw_buffer_load_b128(rd, soff, 16 * i, 0);
         }
-        sl = r < w.rows ? p.lse[(int64_t)(g * G + head) * p.c.Tq + w.t0 + token] : 0.f;
+        {
+            int token, head;
+            cr.split(w.rem + min(tid & (kBM - 1), w.rows - 1), token, head);
+            sl = p.lse[(int64_t)(g * G + head) * p.c.Tq + w.t0 + token];
+        }
         __builtin_amdgcn_sched_barrier(0);
     };
     auto put_stats = [&](int t) {                         // rows behind the last one: zeros, like their Q and dO
@@ -123,235 +181,266 @@ __global__ void __launch_bounds__(kKeysThreads, 1) hyd_cross_bwd_keys_bf16_kerne
         for (int i = 0; i < NV; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc += bf16_lo(so[i][e]) * bf16_lo(sd[i][e]) + bf16_hi(so[i][e]) * bf16_hi(sd[i][e]);
-        acc += __shfl_xor(acc, 1, 64);
-        acc += __shfl_xor(acc, 2, 64);
-        const uint32_t at = lds0 + (uint32_t)(kKeysStatOff + (t & 1) * 2 * kKeysBM * 4 + (tid >> 2) * 4);
-        if ((tid & 3) == 0) {
-            lds_store(at, -sl * kLog2e);
-            lds_store(at + kKeysBM * 4, -acc);
-        }
+#pragma unroll
+        for (int m = 1; m < kPerRow; m <<= 1) acc += __shfl_xor(acc, m, 64);
+        const uint32_t at = lds0 + (uint32_t)(F::kStatOff + (t & 1) * 2 * kBM * 4);
+        if (tid < kBM) lds_store(at + 4 * tid, tid < rows_all - t * kBM ? -sl * kLog2e : 0.f);
+        if (tid % kPerRow == 0) lds_store(at + (kBM + tid / kPerRow) * 4, -acc);
     };
     if (t_lo < t_hi) load_stats(t_lo);
-    // K rows to stage 2, V rows to the place of dS
+    // K rows to the last stage, V rows to the place of dS
     {
         const uint32_t bytes = (uint32_t)(n - 1) * kv_stride_b + kRowB;
-        const uint32_t voff = dma_lane_voff<D>(4 * wave + (lane >> 4), lane, kv_stride_b);
+        const uint32_t voff_kv = dma_lane_voff<D>(4 * wave + (lane >> 4), lane, kv_stride_b);
         auto tile_at = [&](int j) { return (uint32_t)(64 * j) * kv_stride_b; };
-        dma_rows<kKeysWaves>(make_rsrc(p.k + kv_at, bytes), smem + 2 * kKeysStageBytes, [](int j) { return j * 64 * kRowBytes; }, kKeysMax / 64, kv_stride_b, tile_at, wave, voff);
-        dma_rows<kKeysWaves>(make_rsrc(p.v + kv_at, bytes), smem + kKeysDsOff, [](int j) { return j * 64 * kRowBytes; }, kKeysMax / 64, kv_stride_b, tile_at, wave, voff);
+        dma_rows<kKeysWaves>(make_rsrc(p.k + kv_at, bytes), smem + (F::kStages - 1) * F::kStageBytes, [](int j) { return j * 64 * kRowBytes; }, kKeysMax / 64, kv_stride_b, tile_at, wave, voff_kv);
+        dma_rows<kKeysWaves>(make_rsrc(p.v + kv_at, bytes), smem + F::kDsOff, [](int j) { return j * 64 * kRowBytes; }, kKeysMax / 64, kv_stride_b, tile_at, wave, voff_kv);
     }
-    if (t_lo < t_hi) load_tile(t_lo, 0);
-    if (t_lo + 1 < t_hi) load_tile(t_lo + 1, 1);
-    f32x16 dv[NDB], dk[NDB];
+    if (t_lo < t_hi) {
+        load_tile(t_lo, 0);
+        if (F::kStages > 2) load_tile(t_lo + 1, 1);
+    }
+    f32x16 acc[NDB];                                      // dV^T (first waves) or dK^T
 #pragma unroll
     for (int db = 0; db < NDB; ++db)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) dv[db][r] = dk[db][r] = 0.f;
+        for (int r = 0; r < 16; ++r) acc[db][r] = 0.f;
     __builtin_amdgcn_s_waitcnt(0x0F70);                   // vmcnt(0)
     __syncthreads();
-    // this wave's keys, and the columns of K that its dQ takes
-    const bool active = 32 * wave < n;
-    const int cb = D == 128 ? wave : wave & 1, rb0 = D == 128 ? 0 : wave >> 1;
-    constexpr int kRb = D == 128 ? 2 : 1;                 // row blocks of a wave's dQ
-    bf16x8 kf[NK], vf[NK], ktf[kKeysMax / 16];
+    // this wave's operand of the first product, and the columns of K that its dQ takes
+    const int cb = wave % NDB, rb_dq = wave / NDB;        // block of dQ
+    bf16x8 kv[NK], ktf[kKeysMax / 16];
     {
         LdsQueue lq{0};
-        RowFrag f[2 * NK];
+        RowFrag f[NK];
+        const uint32_t at = (uint32_t)((wave < kKeysPairs ? (F::kStages - 1) * F::kStageBytes : F::kDsOff) + 32 * pair * kRowBytes);
 #pragma unroll
-        for (int ks = 0; ks < NK; ++ks) {
-            lds_issue_row(lq, f[ks], fa.row[ks] + (uint32_t)(2 * kKeysStageBytes + 32 * wave * kRowBytes), 0);
-            lds_issue_row(lq, f[NK + ks], fa.row[ks] + (uint32_t)(kKeysDsOff + 32 * wave * kRowBytes), 0);
-        }
+        for (int ks = 0; ks < NK; ++ks) lds_issue_row(lq, f[ks], (row_frag + at) ^ (uint32_t)(ks << 5), 0);
 #pragma unroll
-        for (int ks = 0; ks < NK; ++ks) {
-            lds_wait(lq, f[ks]);
-            kf[ks] = as_bf16x8(f[ks].v ^ sign_flip);      // (only the scores see the sign)
-            vf[ks] = lds_wait(lq, f[NK + ks]);
-        }
-        uint32_t c_lo = fa.col[0], c_hi = fa.col[1];
-#pragma unroll
-        for (int i = 1; i < NDB; ++i)
-            if (cb == i) { c_lo = fa.col[2 * i]; c_hi = fa.col[2 * i + 1]; }
+        for (int ks = 0; ks < NK; ++ks) kv[ks] = as_bf16x8(lds_wait_raw(lq, f[ks]) ^ (wave < kKeysPairs ? sign_flip : 0u));      // (only the scores see the sign)
         ColFrag c[kKeysMax / 16];
 #pragma unroll
-        for (int b = 0; b < kKeysMax / 16; ++b) lds_issue_col(lq, c[b], c_lo + (uint32_t)(2 * kKeysStageBytes), c_hi + (uint32_t)(2 * kKeysStageBytes), b * 16 * kRowBytes);
+        for (int b = 0; b < kKeysMax / 16; ++b) issue_column(lq, c[b], col_frag + (uint32_t)((F::kStages - 1) * F::kStageBytes), cb, b * 16 * kRowBytes);
 #pragma unroll
         for (int b = 0; b < kKeysMax / 16; ++b) ktf[b] = lds_wait(lq, c[b]);
     }
     if (t_lo < t_hi) put_stats(t_lo);
     __builtin_amdgcn_s_waitcnt(0xc07f);                   // lgkmcnt(0)
-    const float hidden = 32 * wave + l32 < n ? 0.f : -INFINITY;       // a key behind the last one: its scores begin, and stay, at -inf
-    // this lane's dS: written by key, read by row
-    const int my_key = 32 * wave + l32;
-    const uint32_t ds_w = lds0 + (uint32_t)(kKeysDsOff + my_key * kKeysDsRow + 8 * half);
-    uint32_t ds_r[kRb][2];
+    const int my_key = 32 * pair + l32;
+    const float hidden = my_key < n ? 0.f : -INFINITY;    // a key behind the last one: its scores begin, and stay, at -inf
+    // this pair's P; this lane's dS, written by key and read by row
+    const uint32_t p_at = lds0 + (uint32_t)(F::kDsOff + 32 * pair * F::kDsRow + 16 * lane);
+    const uint32_t ds_w = lds0 + (uint32_t)(F::kDsOff + my_key * F::kDsRow + 8 * half + (F::swz(my_key) << 5));
+    uint32_t ds_r[2];
 #pragma unroll
-    for (int i = 0; i < kRb; ++i)
-#pragma unroll
-        for (int hi = 0; hi < 2; ++hi) {
-            const int key = 4 * half + 8 * hi + (lane16 >> 2), quarter = 2 * (D == 128 ? i : rb0) + ((lane >> 4) & 1);
-            ds_r[i][hi] = lds0 + (uint32_t)(kKeysDsOff + key * kKeysDsRow + ((quarter ^ ds_swz(key)) << 5) + 8 * (lane16 & 3));
-        }
+    for (int hi = 0; hi < 2; ++hi) {
+        const int key = 4 * half + 8 * hi + (lane16 >> 2), quarter = 2 * rb_dq + ((lane >> 4) & 1);
+        ds_r[hi] = lds0 + (uint32_t)(F::kDsOff + key * F::kDsRow + ((quarter ^ F::swz(key)) << 5) + 8 * (lane16 & 3));
+    }
 
-    for (int t = t_lo; t < t_hi; ++t) {
-        const int stage = (t - t_lo) % kKeysStages, base = stage * kKeysStageBytes;
-        // this tile is there: at most the next one's loads are under way (stores of dQ only make the wait stricter)
-        if (t + 1 < t_hi) __builtin_amdgcn_s_waitcnt(0x0F70 | (kDma & 15));
-        else __builtin_amdgcn_s_waitcnt(0x0F70);
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        if (t + 1 < t_hi) load_stats(t + 1);
-        if (t + 2 < t_hi) load_tile(t + 2, stage == 0 ? 2 : stage - 1);
-        __builtin_amdgcn_sched_barrier(0);
-        {   // (a wave without keys goes along: its P and dS are zeros, and a branch here costs copies of the accumulators)
-            const uint32_t qt = (uint32_t)base, stat = lds0 + (uint32_t)(kKeysStatOff + (t & 1) * 2 * kKeysBM * 4 + 16 * half);
-#pragma unroll
-            for (int rb = 0; rb < 2; ++rb) {
-                // fragments are read kAhead ahead: Q and dO rows, then dO and Q columns
-                constexpr int kAhead = 4;
-                LdsQueue lq{0};
-                RowFrag f[kAhead], l4[4], d4[4];
-                ColFrag cf[kAhead];
-                f32x16 s, xd;
-                uint32_t ph[8], pl[8], sh[8], sl2[8];
+    // (each role runs its own copy of the tile loop, so that no register has to be reconciled where their paths would join)
+    auto tiles = [&](auto role_tag) {
+        constexpr bool kB = decltype(role_tag)::value;
+        constexpr int kAhead = 4;
+        for (int t = t_lo; t < t_hi; ++t) {
+            const int stage = (t - t_lo) % F::kStages, base = stage * F::kStageBytes;
+            // this tile is there, and what was written behind the last barrier: at most the next one's loads are under way (stores of dQ
+            // only make the wait stricter)
+            __builtin_amdgcn_s_waitcnt(0x0070 | (F::kStages > 2 ? kDma & 15 : 0));
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            auto load_next = [&]() {
+                load_stats(t + 1);
+                load_tile(t + F::kStages - 1, stage == 0 ? F::kStages - 1 : stage - 1);
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            const uint32_t qt = (uint32_t)base, stat = lds0 + (uint32_t)(F::kStatOff + (t & 1) * 2 * kBM * 4 + 16 * half);
+            f32x16 x1[kBlocks];                           // S and P, or dP
+            LdsQueue lq{0};
+            ColFrag cf[kAhead];
+            // fragment i of the second product: (row block, 16 rows of it, column block)
+            uint32_t row_at = row_frag + qt, col_at = col_frag + qt;
+            auto issue_second = [&](int i) {
+                const int rb = i / (2 * NDB), j = i % (2 * NDB);
+                if (j == 0) asm volatile("" : "+v"(col_at));                  // (addresses of one block at a time)
+                issue_column(lq, cf[i % kAhead], col_at, j % NDB + (rb >> 1) * NDB, (kB ? 0 : F::kTileBytes) + (2 * (rb & 1) + j / NDB) * 16 * kRowBytes);
+            };
+            {
+                RowFrag f[kAhead], st[4];
                 auto issue_first = [&](int i) {
-                    lds_issue_row(lq, f[i % kAhead], fa.row[i % NK] + qt, (i < NK ? 0 : kKeysTileBytes) + 32 * rb * kRowBytes);
+                    if (i % NK == 0) asm volatile("" : "+v"(row_at));
+                    lds_issue_row(lq, f[i % kAhead], row_at ^ (uint32_t)((i % NK + i / NK / 2 * NK) << 5), (kB ? F::kTileBytes : 0) + 32 * (i / NK % 2) * kRowBytes);
                 };
-                auto issue_second = [&](int i) {
-                    const int j = i % (2 * NDB);
-                    lds_issue_col(lq, cf[i % kAhead], fa.col[2 * (j % NDB)] + qt, fa.col[2 * (j % NDB) + 1] + qt, (i < 2 * NDB ? kKeysTileBytes : 0) + (2 * rb + j / NDB) * 16 * kRowBytes);
+                // statistics of a row block: -D starts dP, -LSE2 is needed when the scores are there
+                auto issue_stat = [&](int rb, int rq) { lds_issue_row(lq, st[rq], stat, ((kB ? kBM : 0) + 32 * rb + 8 * rq) * 4); };
+                auto form_p = [&](int rb, int rq) {
+                    const u32x4 v = lds_wait_raw(lq, st[rq]);
+                    u32x4 w;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        x1[rb][4 * rq + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x1[rb][4 * rq + e], scale_log2, __uint_as_float(v[e])));
+                        w[e] = __float_as_uint(x1[rb][4 * rq + e]);
+                    }
+                    lds_store(p_at, w, F::p_off(rb) + rq * 1024);
+                    ++lq.issued;
                 };
+#pragma unroll
+                for (int rq = 0; rq < 4; ++rq) issue_stat(0, rq);
 #pragma unroll
                 for (int i = 0; i < kAhead; ++i) issue_first(i);
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = hidden;
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int i = 0; i < NK; ++i) {            // S
-                    s = mfma32(lds_wait(lq, f[i % kAhead]), kf[i], s);
-                    issue_first(i + kAhead);
-                    if (i < 4) lds_issue_row(lq, d4[i], stat, (kKeysBM + 32 * rb + 8 * i) * 4);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
+                for (int rb = 0; rb < kBlocks; ++rb) {
+                    if (kB) {
 #pragma unroll
-                for (int rq = 0; rq < 4; ++rq) {          // dP begins at -D
-                    const u32x4 v = lds_wait_raw(lq, d4[rq]);
+                        for (int rq = 0; rq < 4; ++rq) {
+                            const u32x4 v = lds_wait_raw(lq, st[rq]);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) xd[4 * rq + e] = __uint_as_float(v[e]);
-                }
+                            for (int e = 0; e < 4; ++e) x1[rb][4 * rq + e] = __uint_as_float(v[e]);
+                        }
+                        if (rb + 1 < kBlocks) {
 #pragma unroll
-                for (int rq = 0; rq < 4; ++rq) lds_issue_row(lq, l4[rq], stat, (32 * rb + 8 * rq) * 4);
-                __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                for (int i = 0; i < NK; ++i) {            // dP
-                    xd = mfma32(lds_wait(lq, f[i % kAhead]), vf[i], xd);
-                    if (i + kAhead < NK) issue_first(NK + i + kAhead);
-                    else issue_second(i + kAhead - NK);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-#pragma unroll
-                for (int rq = 0; rq < 4; ++rq) {          // P in place of S
-                    const u32x4 v = lds_wait_raw(lq, l4[rq]);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s[4 * rq + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * rq + e], scale_log2, __uint_as_float(v[e])));
-                }
-#pragma unroll
-                for (int j = 0; j < 8; ++j) split_bf16(s[2 * j], s[2 * j + 1], ph[j], pl[j]);
-                __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                for (int i = 0; i < 4 * NDB; ++i) {       // dV, then dK; dS is formed under the first products of dV
-                    const int j = i % (2 * NDB), b2 = j / NDB, db = j % NDB;
-                    const bf16x8 a = lds_wait(lq, cf[i % kAhead]);
-                    const auto frag = [&](const uint32_t (&w)[8]) { return as_bf16x8(u32x4{w[4 * b2], w[4 * b2 + 1], w[4 * b2 + 2], w[4 * b2 + 3]}); };
-                    if (i < 2 * NDB) {
-                        dv[db] = mfma32(a, frag(ph), dv[db]);
-                        dv[db] = mfma32(a, frag(pl), dv[db]);
+                            for (int rq = 0; rq < 4; ++rq) issue_stat(rb + 1, rq);
+                        }
                     } else {
-                        dk[db] = mfma32(a, frag(sh), dk[db]);
-                        dk[db] = mfma32(a, frag(sl2), dk[db]);
-                    }
-                    if (i + kAhead < 4 * NDB) issue_second(i + kAhead);
-                    constexpr int kPer = 8 / (2 * NDB);   // pairs of dS formed beside a fragment of dO
 #pragma unroll
-                    for (int e = 0; e < kPer; ++e) {
-                        const int m = kPer * i + e;
-                        if (i < 2 * NDB) split_bf16(s[2 * m] * xd[2 * m], s[2 * m + 1] * xd[2 * m + 1], sh[m], sl2[m]);
+                        for (int r = 0; r < 16; ++r) x1[rb][r] = hidden;
                     }
-                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int i = 0; i < NK; ++i) {        // (a block's probabilities are formed under the next one's scores)
+                        const int m = NK * rb + i;
+                        x1[rb] = mfma32(lds_wait(lq, f[m % kAhead]), kv[i], x1[rb]);
+                        if (m + kAhead < kBlocks * NK) issue_first(m + kAhead);
+                        __builtin_amdgcn_sched_barrier(0);
+                        if (!kB && rb > 0) {
+                            constexpr int kEvery = NK / 4;
+                            if (i % kEvery == kEvery - 1) {
+                                form_p(rb - 1, i / kEvery);
+                                issue_stat(rb, i / kEvery);
+                            }
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+                    }
                 }
+                if (!kB) {
 #pragma unroll
-                for (int rq = 0; rq < 4; ++rq) {          // rows 32 rb + 8 rq + 4 half ..: quarter 2 rb + rq / 2
-                    const uint32_t at = ds_w + (uint32_t)(((2 * rb + (rq >> 1)) ^ ds_swz(my_key)) << 5) + 16 * (rq & 1);
-                    lds_store(at, u32x2{sh[2 * rq], sh[2 * rq + 1]});
-                    lds_store(at + kKeysDsBytes, u32x2{sl2[2 * rq], sl2[2 * rq + 1]});
+                    for (int rq = 0; rq < 4; ++rq) form_p(kBlocks - 1, rq);
                 }
             }
-        }
-        if (t + 1 < t_hi) put_stats(t + 1);
-        __builtin_amdgcn_s_waitcnt(0xc07f);               // lgkmcnt(0): dS and the statistics are written, Q and dO read
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        // dQ^T = K^T dS^T, 32 columns of the head
-        f32x16 dq[kRb];
 #pragma unroll
-        for (int i = 0; i < kRb; ++i)
+            for (int i = 0; i < kAhead; ++i) issue_second(i);
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_waitcnt(0xc07f | ((2 * kAhead) << 8));         // LDS operations complete in order: P is written
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            load_next();                                  // (here and not at the top: fewer registers through the first products)
+            if constexpr (kB) {                           // dS in place of dP; all of P is read before dS takes its place
 #pragma unroll
-            for (int r = 0; r < 16; ++r) dq[i][r] = 0.f;
-        {
-            constexpr int kAhead = 4, kFrags = kKeysMax / 16 * 2 * kRb;      // fragment m: 16 keys, hi or lo, row block
-            LdsQueue lq{0};
-            ColFrag f[kAhead];
-            auto issue = [&](int m) {
-                const int i = m % kRb, lo = m / kRb % 2, b = m / kRb / 2;
-                lds_issue_col(lq, f[m % kAhead], ds_r[i][0], ds_r[i][1], lo * kKeysDsBytes + b * 16 * kKeysDsRow);
+                for (int rb = 0; rb < kBlocks; ++rb) {
+                    LdsQueue lp{0};
+                    RowFrag f[4];
+#pragma unroll
+                    for (int rq = 0; rq < 4; ++rq) lds_issue_row(lp, f[rq], p_at, F::p_off(rb) + rq * 1024);
+#pragma unroll
+                    for (int rq = 0; rq < 4; ++rq) {
+                        const u32x4 v = lds_wait_raw(lp, f[rq]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x1[rb][4 * rq + e] *= __uint_as_float(v[e]);
+                    }
+                }
+            }
+            // The second product, in groups of 16 rows.  A group's operand is formed under the products of the one before it.
+            uint32_t hi[2][4], lo[2][4], ds_at = ds_w;
+            asm volatile("" : "+v"(ds_at));               // (the addresses that follow from it are formed here, not kept through the loop)
+            auto form = [&](int q, int m) {               // pair m of group q
+                const int r = 8 * (q & 1) + 2 * m;
+                split_bf16(x1[q >> 1][r], x1[q >> 1][r + 1], hi[q & 1][m], lo[q & 1][m]);
+                if (kB && (m & 1)) {                      // dS of rows 32 rb + 8 rq + 4 half ..
+                    const int rb = q >> 1, rq = 2 * (q & 1) + (m >> 1);
+                    const uint32_t at = (ds_at ^ (uint32_t)((2 * rb + (rq >> 1)) << 5)) + 16 * (rq & 1);
+                    lds_store(at, u32x2{hi[q & 1][m - 1], hi[q & 1][m]});
+                    lds_store(at + F::kDsBytes, u32x2{lo[q & 1][m - 1], lo[q & 1][m]});
+                    lq.issued += 2;
+                }
             };
+            lq.issued = 2 * kAhead;                       // (the reads from before the barrier, restated; B's have been waited for)
 #pragma unroll
-            for (int m = 0; m < kAhead; ++m) issue(m);
+            for (int i = 0; i < kAhead; ++i) cf[i].seq = 2 * (i + 1);
 #pragma unroll
-            for (int m = 0; m < kFrags; ++m) {
-                dq[m % kRb] = mfma32(ktf[m / kRb / 2], lds_wait(lq, f[m % kAhead]), dq[m % kRb]);
-                if (m + kAhead < kFrags) issue(m + kAhead);
+            for (int m = 0; m < 4; ++m) form(0, m);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < kBlocks * 2 * NDB; ++i) {
+                const int q = i / NDB, db = i % NDB;
+                const bf16x8 a = lds_wait(lq, cf[i % kAhead]);
+                const uint32_t (&h)[4] = hi[q & 1], (&l)[4] = lo[q & 1];
+                acc[db] = mfma32(a, as_bf16x8(u32x4{h[0], h[1], h[2], h[3]}), acc[db]);
+                acc[db] = mfma32(a, as_bf16x8(u32x4{l[0], l[1], l[2], l[3]}), acc[db]);
+                if (i + kAhead < kBlocks * 2 * NDB) issue_second(i + kAhead);
+                constexpr int kPer = 4 / NDB;
+#pragma unroll
+                for (int e = 0; e < kPer; ++e)
+                    if (q + 1 < 2 * kBlocks) form(q + 1, kPer * db + e);
                 __builtin_amdgcn_sched_barrier(0);
             }
-        }
-        // through this wave's part of the stage (its Q and dO have been read), then 64 bytes of each row
-        const Rows w = tile_rows(t);
-        const uint32_t out = lds0 + (uint32_t)(base + wave * kKeysBM * kKeysOutRow);
+            __builtin_amdgcn_s_waitcnt(0xc07f);           // lgkmcnt(0): dS is written, Q and dO read
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            put_stats(t + 1);                             // (the next barrier publishes them)
+            f32x16 dq;
 #pragma unroll
-        for (int i = 0; i < kRb; ++i)
+            for (int r = 0; r < 16; ++r) dq[r] = 0.f;
+            {
+                constexpr int kFrags = kKeysMax / 16 * 2; // fragment m: 16 keys, hi or lo
+                LdsQueue ld{0};
+                ColFrag f[kAhead];
+                auto issue = [&](int m) { lds_issue_col(ld, f[m % kAhead], ds_r[0], ds_r[1], (m & 1) * F::kDsBytes + (m >> 1) * 16 * F::kDsRow); };
+#pragma unroll
+                for (int m = 0; m < kAhead; ++m) issue(m);
+#pragma unroll
+                for (int m = 0; m < kFrags; ++m) {
+                    dq = mfma32(ktf[m >> 1], lds_wait(ld, f[m % kAhead]), dq);
+                    if (m + kAhead < kFrags) issue(m + kAhead);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            // through this wave's part of the stage (its Q and dO have been read), then 64 bytes of each row
+            const KeysRows w = tile_rows(t);
+            const uint32_t out = lds0 + (uint32_t)(base + wave * 32 * kKeysOutRow);
+            int ln = lane;
+            asm volatile("" : "+v"(ln));                  // (likewise)
 #pragma unroll
             for (int rq = 0; rq < 4; ++rq)
-                lds_store(out + (uint32_t)((32 * i + l32) * kKeysOutRow + (8 * rq + 4 * half) * 2),
-                          u32x2{pack_bf16(dq[i][4 * rq] * p.scale, dq[i][4 * rq + 1] * p.scale), pack_bf16(dq[i][4 * rq + 2] * p.scale, dq[i][4 * rq + 3] * p.scale)});
-        __builtin_amdgcn_s_waitcnt(0xc07f);
-        {
-            LdsQueue lq{0};
-            RowFrag f[2 * kRb];
+                lds_store(out + (uint32_t)((ln & 31) * kKeysOutRow + (8 * rq + 4 * (ln >> 5)) * 2),
+                          u32x2{pack_bf16(dq[4 * rq] * p.scale, dq[4 * rq + 1] * p.scale), pack_bf16(dq[4 * rq + 2] * p.scale, dq[4 * rq + 3] * p.scale)});
+            __builtin_amdgcn_s_waitcnt(0xc07f);
+            {
+                LdsQueue ld{0};
+                RowFrag f[2];
 #pragma unroll
-            for (int i = 0; i < 2 * kRb; ++i) lds_issue_row(lq, f[i], out + (uint32_t)((lane >> 2) * kKeysOutRow + (lane & 3) * 16), 16 * i * kKeysOutRow);
+                for (int i = 0; i < 2; ++i) lds_issue_row(ld, f[i], out + (uint32_t)((ln >> 2) * kKeysOutRow + (ln & 3) * 16), 16 * i * kKeysOutRow);
 #pragma unroll
-            for (int i = 0; i < 2 * kRb; ++i) {
-                const u32x4 v = lds_wait_raw(lq, f[i]);
-                const int r = 32 * rb0 + 16 * i + (lane >> 2);
-                int token, head;
-                cr.split(w.rem + r, token, head);
-                if (r < w.rows)
-                    *reinterpret_cast<u32x4*>(p.dq + (int64_t)(w.t0 + token) * q_stride + (int64_t)(g * G + head) * D + 32 * cb + 8 * (lane & 3)) = v;
+                for (int i = 0; i < 2; ++i) {
+                    const u32x4 v = lds_wait_raw(ld, f[i]);
+                    const int r = 32 * rb_dq + 16 * i + (ln >> 2);
+                    int token, head;
+                    cr.split(w.rem + r, token, head);
+                    if (r < w.rows)
+                        *reinterpret_cast<u32x4*>(p.dq + (int64_t)(w.t0 + token) * q_stride + (int64_t)(g * G + head) * D + 32 * cb + 8 * (ln & 3)) = v;
+                }
             }
         }
-    }
+    };
+    if (wave >= kKeysPairs) tiles(std::true_type{});
+    else tiles(std::false_type{});
     __syncthreads();                                      // every wave is done with the ring
-    if (active) {
-        const uint32_t o_stage = lds0 + (uint32_t)(wave * 2 * 32 * kRowBytes);
-        const int64_t at = kv_at + (int64_t)(32 * wave) * kv_stride;
-        if (p.parts == 1) {
-            store_rows_via_lds<D>(p.dv + at, kv_stride, n - 32 * wave, dv, 1.f, o_stage, lane);
-            store_rows_via_lds<D>(p.dk + at, kv_stride, n - 32 * wave, dk, p.scale, o_stage + 32 * kRowBytes, lane);
-        } else {
-            const int64_t plane = (int64_t)p.c.Tk * kv_stride;
-            store_rows_f32_via_lds<D>(p.part + (p.parts + part) * plane + at, kv_stride, n - 32 * wave, dv, 1.f, o_stage, lane);
-            store_rows_f32_via_lds<D>(p.part + part * plane + at, kv_stride, n - 32 * wave, dk, p.scale, o_stage + 32 * kRowBytes, lane);
-        }
+    if (32 * pair < n) {
+        const uint32_t o_stage = lds0 + (uint32_t)(wave * 32 * kRowBytes);
+        const int64_t at = kv_at + (int64_t)(32 * pair) * kv_stride;
+        const bool is_k = wave >= kKeysPairs;
+        const float mul = is_k ? p.scale : 1.f;
+        if (p.parts == 1) store_rows_via_lds<D>((is_k ? p.dk : p.dv) + at, kv_stride, n - 32 * pair, acc, mul, o_stage, lane);
+        else store_rows_f32_via_lds<D>(p.part + ((is_k ? 0 : p.parts) + part) * (int64_t)p.c.Tk * kv_stride + at, kv_stride, n - 32 * pair, acc, mul, o_stage, lane);
     }
 }
 
