@@ -89,7 +89,7 @@ BwdLayout bwd_layout(const Sizes& z) {
     w.n_q = most_tiles((long long)z.Tq * G, (long long)z.max_q * G, z.nseq, tile_q(z.dt));
     w.n_kv = most_tiles(z.Tk, z.max_kv, z.nseq, tile_kv(z.dt));
     const size_t q_elems = (size_t)z.Tq * z.hq * z.d, kv_elems = (size_t)z.Tk * z.hkv * z.d;
-    const auto records = [](long long n) { return align_up(16 * (size_t)(n > kBwdItems ? n : kBwdItems)); };      // (parts: kBwdItems records at most)
+    const auto records = [](long long n) { return align_up(16 * (size_t)(n > kCus ? n : kCus)); };      // (in parts: kCus records at most)
     size_t at = 0;
     w.q_hdr = at;    at += align_up(sizeof(int) * kHdrTotal);
     w.q_items = at;  at += records(w.n_q);
@@ -97,14 +97,13 @@ BwdLayout bwd_layout(const Sizes& z) {
     w.kv_items = at; at += records(w.n_kv);
     if (z.dt == HYD_FP32) {
         w.stat[0] = at; at += align_up(sizeof(float) * (size_t)z.Tq * z.hq);
-        w.need = w.total = at;
-        return w;
+    } else {
+        for (size_t& s : w.stat) { s = at; at += align_up(sizeof(float) * (size_t)z.Tq * z.hq); }
+        w.q16 = at;      at += align_up(2 * q_elems);
+        w.do16 = at;     at += align_up(2 * q_elems);
+        w.k16 = at;      at += align_up(2 * kv_elems);
+        w.absmax = at;   at += align_up(sizeof(uint32_t) * kPrepMaxWg);
     }
-    for (size_t& s : w.stat) { s = at; at += align_up(sizeof(float) * (size_t)z.Tq * z.hq); }
-    w.q16 = at;      at += align_up(2 * q_elems);
-    w.do16 = at;     at += align_up(2 * q_elems);
-    w.k16 = at;      at += align_up(2 * kv_elems);
-    w.absmax = at;   at += align_up(sizeof(uint32_t) * kPrepMaxWg);
     w.need = at;
     const size_t q_rows = (size_t)z.Tq * z.hq * kBwdMaxParts, kv_rows = (size_t)z.Tk * z.hkv * kBwdMaxParts;
     const size_t dq = (q_rows < kDqPartRows ? q_rows : kDqPartRows) * (size_t)z.d * 4, dkv = (kv_rows < kKvPartRows ? kv_rows : kKvPartRows) * (size_t)z.d * 8;
@@ -137,7 +136,8 @@ bool prep_kernels() {
            allow_lds(hyd_cross_bwd_keys_bf16_kernel<D>, KeysForm<D>::kLds) &&
            allow_lds(hyd_bwd_dkdv_wide_bf16_kernel<D, CrossBwdParams>, kKwLds) && allow_lds(hyd_cross_fwd_fp32_kernel<D, false>, f32_lds<D>()) &&
            allow_lds(hyd_cross_fwd_fp32_kernel<D, true>, f32_lds<D>()) && allow_lds(hyd_cross_dq_fp32_kernel<D>, f32_lds<D>()) &&
-           allow_lds(hyd_cross_dkdv_fp32_kernel<D>, f32_lds<D>());
+           allow_lds(hyd_cross_dkdv_fp32_kernel<D, false>, f32_lds<D>()) &&
+           allow_lds(hyd_cross_dkdv_fp32_kernel<D, true>, f32_lds<D>());
 }
 hyd_status cross_device(int* cus) {
     int dev = 0;
@@ -240,9 +240,9 @@ void launch_fwd(const Sizes& z, const CrossShape& c, const void* q, const void* 
 }
 
 template <int D>
-void launch_sum(const CrossSum& x, hipStream_t st) {
+void launch_sum(const CrossSum& x, bool f32, hipStream_t st) {
     KernelTimer kt("cross_sum", st);
-    hipLaunchKernelGGL(hyd_cross_sum_kernel<D>, dim3((unsigned)x.T, x.out[1] ? 2 : 1), dim3(kCrossSumThreads), 0, st, x);
+    hipLaunchKernelGGL((f32 ? hyd_cross_sum_kernel<D, true> : hyd_cross_sum_kernel<D, false>), dim3((unsigned)x.T, x.out[1] ? 2 : 1), dim3(kCrossSumThreads), 0, st, x);
 }
 
 struct BwdArgs { const void *q, *k, *v, *o; const float* lse; const void* d_o; void *dq, *dk, *dv; };
@@ -273,7 +273,7 @@ void launch_bwd(const Sizes& z, const CrossShape& c, const BwdArgs& a, float sca
             hipLaunchKernelGGL(hyd_cross_bwd_keys_bf16_kernel<D>, dim3((unsigned)(items * p.parts)), dim3(kKeysThreads), KeysForm<D>::kLds, st, p);
         }
         if (p.parts > 1)
-            launch_sum<D>(CrossSum{part, {p.dk, p.dv}, c.cu_kv, c.kv_lens, z.nseq, z.Tk, z.hkv, p.parts}, st);
+            launch_sum<D>(CrossSum{part, {p.dk, p.dv}, c.cu_kv, c.kv_lens, z.nseq, z.Tk, z.hkv, p.parts}, false, st);
         return;
     }
     int* q_hdr = reinterpret_cast<int*>(ws + w.q_hdr); int* kv_hdr = reinterpret_cast<int*>(ws + w.kv_hdr);
@@ -307,7 +307,7 @@ void launch_bwd(const Sizes& z, const CrossShape& c, const BwdArgs& a, float sca
         KernelTimer kt("cross_dq", st);
         hipLaunchKernelGGL(hyd_cross_dq_bf16_kernel<D>, dim3(grid), dim3(kDqThreads), kDqLds, st, p, l);
     }
-    if (parts_q > 1) launch_sum<D>(CrossSum{part, {static_cast<uint16_t*>(a.dq), nullptr}, c.cu_q, nullptr, z.nseq, z.Tq, z.hq, parts_q}, st);
+    if (parts_q > 1) launch_sum<D>(CrossSum{part, {a.dq, nullptr}, c.cu_q, nullptr, z.nseq, z.Tq, z.hq, parts_q}, false, st);
     if (z.Tk == 0) return;
     {
         CrossBwdParams p;
@@ -324,26 +324,30 @@ void launch_bwd(const Sizes& z, const CrossShape& c, const BwdArgs& a, float sca
         hipLaunchKernelGGL((hyd_bwd_dkdv_wide_bf16_kernel<D, CrossBwdParams>), dim3(grid), dim3(kKwThreads), kKwLds, st, p, l);
     }
     if (parts_kv > 1)
-        launch_sum<D>(CrossSum{part, {static_cast<uint16_t*>(a.dk), static_cast<uint16_t*>(a.dv)}, c.cu_kv, c.kv_lens, z.nseq, z.Tk, z.hkv, parts_kv}, st);
+        launch_sum<D>(CrossSum{part, {a.dk, a.dv}, c.cu_kv, c.kv_lens, z.nseq, z.Tk, z.hkv, parts_kv}, false, st);
 }
 
 template <int D>
-void launch_bwd_f32(const Sizes& z, const CrossShape& c, const BwdArgs& a, float scale, char* ws, size_t, int cus, hipStream_t st) {
+void launch_bwd_f32(const Sizes& z, const CrossShape& c, const BwdArgs& a, float scale, char* ws, size_t ws_bytes, int cus, hipStream_t st) {
     const BwdLayout w = bwd_layout(z);
+    float* part = reinterpret_cast<float*>(ws + w.need);
+    const size_t room = ws_bytes - w.need, q_rows = (size_t)z.Tq * z.hq, kv_rows = (size_t)z.Tk * z.hkv;
+    const int parts_q = bwd_parts(w.n_q * z.hkv, kCus, tiles(z.max_kv, kF32Tile), 1, q_rows, kDqPartRows, (size_t)D * 4, room);
+    const int parts_kv = bwd_parts(w.n_kv * z.hkv, kCus, tiles(z.max_q, kF32Tile) * c.G, 2, kv_rows, kKvPartRows, (size_t)D * 8, room);
     int* hdr[2] = {reinterpret_cast<int*>(ws + w.q_hdr), reinterpret_cast<int*>(ws + w.kv_hdr)};
     int* items[2] = {reinterpret_cast<int*>(ws + w.q_items), reinterpret_cast<int*>(ws + w.kv_items)};
     {
         CrossF32Begin b;
         b.c = c; b.dk = static_cast<float*>(a.dk); b.dv = static_cast<float*>(a.dv); b.d = D;
-        b.lists[0] = CrossList{hdr[0], items[0], kF32BM, 1, (int)w.n_q, false};
-        b.lists[1] = CrossList{hdr[1], items[1], kF32KvBN, 1, (int)w.n_kv, true};
+        b.lists[0] = CrossList{hdr[0], items[0], kF32BM, parts_q, (int)(w.n_q * parts_q), false};
+        b.lists[1] = CrossList{hdr[1], items[1], kF32KvBN, parts_kv, (int)(w.n_kv * parts_kv), true};
         const int n_zero = !c.kv_lens ? 0 : (z.nseq < kCus ? z.nseq : kCus);
         KernelTimer kt("cross_begin", st);
         hipLaunchKernelGGL(hyd_cross_begin_fp32_kernel, dim3(2 + n_zero), dim3(kPreludeThreads), kCrossListLds, st, b);
     }
     CrossF32Params p;
     memset(&p, 0, sizeof(p));
-    p.c = c; p.scale = scale; p.parts = 1;
+    p.c = c; p.scale = scale; p.part_o = part;
     p.q = static_cast<const float*>(a.q); p.k = static_cast<const float*>(a.k); p.v = static_cast<const float*>(a.v);
     p.o = static_cast<const float*>(a.o); p.d_o = static_cast<const float*>(a.d_o); p.lse_in = a.lse;
     p.dq = static_cast<float*>(a.dq); p.dk = static_cast<float*>(a.dk); p.dv = static_cast<float*>(a.dv);
@@ -354,13 +358,19 @@ void launch_bwd_f32(const Sizes& z, const CrossShape& c, const BwdArgs& a, float
         return grid;
     };
     {
-        const int grid = take(0, w.n_q * z.hkv);
+        const int grid = take(0, w.n_q * z.hkv * parts_q);
+        p.parts = parts_q;
         KernelTimer kt("cross_dq", st);
         hipLaunchKernelGGL(hyd_cross_dq_fp32_kernel<D>, dim3(grid), dim3(64 * kF32Waves), f32_lds<D>(), st, p);
     }
-    const int grid = take(1, w.n_kv * z.hkv);
-    KernelTimer kt("cross_dkdv", st);
-    hipLaunchKernelGGL(hyd_cross_dkdv_fp32_kernel<D>, dim3(grid), dim3(64 * kF32KvWaves), f32_lds<D>(), st, p);
+    if (parts_q > 1) launch_sum<D>(CrossSum{part, {a.dq, nullptr}, c.cu_q, nullptr, z.nseq, z.Tq, z.hq, parts_q}, true, st);
+    const int grid = take(1, w.n_kv * z.hkv * parts_kv);
+    p.parts = parts_kv;
+    {
+        KernelTimer kt("cross_dkdv", st);
+        hipLaunchKernelGGL((parts_kv > 1 ? hyd_cross_dkdv_fp32_kernel<D, true> : hyd_cross_dkdv_fp32_kernel<D, false>), dim3(grid), dim3(64 * kF32KvWaves), f32_lds<D>(), st, p);
+    }
+    if (parts_kv > 1) launch_sum<D>(CrossSum{part, {a.dk, a.dv}, c.cu_kv, c.kv_lens, z.nseq, z.Tk, z.hkv, parts_kv}, true, st);
 }
 
 // What both directions check before any HIP call; HYD_OK with *nothing set: there is nothing to do.

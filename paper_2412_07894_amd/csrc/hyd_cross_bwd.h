@@ -350,11 +350,11 @@ __global__ void __launch_bounds__(kDqThreads, 1) hyd_cross_dq_bf16_kernel(CrossD
 // ---------------------------------------------------------------------------------------------
 constexpr int kCrossSumThreads = 256;
 struct CrossSum {
-    const float* part; uint16_t* out[2];          // [outputs][parts] planes
+    const float* part; void* out[2];              // [outputs][parts] planes
     const int32_t* cu; const int32_t* lens;       // lens: NULL, or valid rows of a sequence
     int nseq, T, heads, parts;
 };
-template <int D>
+template <int D, bool kF32>
 __global__ void __launch_bounds__(kCrossSumThreads) hyd_cross_sum_kernel(CrossSum p) {
     const int t = blockIdx.x;
     if (t < p.cu[0] || t >= p.cu[p.nseq]) return;
@@ -367,7 +367,8 @@ __global__ void __launch_bounds__(kCrossSumThreads) hyd_cross_sum_kernel(CrossSu
         const float* src = p.part + blockIdx.y * (int64_t)p.parts * plane + t * row + i;
         f32x4 sum = *reinterpret_cast<const f32x4*>(src);
         for (int x = 1; x < p.parts; ++x) sum += *reinterpret_cast<const f32x4*>(src + x * plane);
-        *reinterpret_cast<u32x2*>(p.out[blockIdx.y] + t * row + i) = u32x2{pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3])};
+        if (kF32) *reinterpret_cast<f32x4*>(static_cast<float*>(p.out[blockIdx.y]) + t * row + i) = sum;
+        else *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.out[blockIdx.y]) + t * row + i) = u32x2{pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3])};
     }
 }
 

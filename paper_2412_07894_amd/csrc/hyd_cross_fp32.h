@@ -17,8 +17,8 @@ struct CrossF32Params {
     float scale;
     const int* hdr; int* cursors; const int* items;
     HeadMap hm;
-    int parts, tiles;                     // forward: parts of the keys; own items: tiles of a sequence at most
-    float* part_o; float* part_lse;
+    int parts, tiles;                     // parts of an item; forward, own items: tiles of a sequence at most
+    float* part_o; float* part_lse;       // forward: see CrossJoin; backward: part_o holds the planes that are summed
 };
 
 // Item lists of the backward (workgroups 0 and 1), zeros in dK and dV behind the valid keys (the others).
@@ -37,6 +37,13 @@ __global__ void __launch_bounds__(kPreludeThreads) hyd_cross_begin_fp32_kernel(C
             *reinterpret_cast<f32x4*>(p.dv + 4 * i) = f32x4{0.f, 0.f, 0.f, 0.f};
         }
     }
+}
+
+// LDS reads of this wave done (before a barrier after which the tile may be overwritten)
+__device__ __forceinline__ void f32_wait_lds() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xc07f);
+    asm volatile("" ::: "memory");
 }
 
 // Where the packed rows of an item lie in the caller's tensors.
@@ -213,16 +220,18 @@ __global__ void __launch_bounds__(64 * kF32Waves, 1) hyd_cross_dq_fp32_kernel(Cr
     WorkFetcher wf;
     WorkItem wi;
     for (bool have = wf.first(p.hm, p.hdr, p.cursors, p.items, slot, wi, blockIdx.x); have; have = wf.next(p.hm, p.cursors, p.items, slot, wi)) {
-        const int g = wi.head, rows = wi.lev, n = wi.len;
+        const int g = wi.head, rows = wi.lev & ((1 << kCrossPartShift) - 1), part = wi.lev >> kCrossPartShift, n = wi.len;
         const CrossF32Rows at(p.c, wi.seq, g, D);
         const int wrow0 = 32 * rg, i = wrow0 + l32;
-        const int n_kt = (n + kF32Tile - 1) / kF32Tile;
-        if (n_kt == 0) {
+        const int n_all = (n + kF32Tile - 1) / kF32Tile, per_part = (n_all + p.parts - 1) / p.parts;
+        const int t_lo = min(part * per_part, n_all), n_kt = min(t_lo + per_part, n_all);      // (the first part has tiles if there are any)
+        float* const out = p.parts > 1 ? p.part_o + (int64_t)part * p.c.Tq * p.c.hq * D : p.dq;
+        if (t_lo == n_kt) {
             wf.claim(p.hm, p.cursors);
             if (split == 0 && i < rows) {
                 f32x16 z[NDB];
                 f32_zero(z);
-                f32_store_row<D>(p.dq + at.at(i), z, 0.f, half);
+                f32_store_row<D>(out + at.at(i), z, 0.f, half);
             }
             continue;
         }
@@ -230,7 +239,8 @@ __global__ void __launch_bounds__(64 * kF32Waves, 1) hyd_cross_dq_fp32_kernel(Cr
         const __amdgpu_buffer_rsrc_t rk = make_rsrc(p.k + ((int64_t)wi.row0 * p.c.hkv + g) * D, kv_bytes);
         const __amdgpu_buffer_rsrc_t rv = make_rsrc(p.v + ((int64_t)wi.row0 * p.c.hkv + g) * D, kv_bytes);
         const int64_t roff = at.at(min(i, rows - 1)), soff = at.stat(min(i, rows - 1));
-        fl.load(rk, smem, 0, stride_b);
+        const uint32_t first = (uint32_t)t_lo * kF32Tile * stride_b;
+        fl.load(rv, smem + kT, first, stride_b);
         f32x4 q[D / 8], dof[D / 8];
         f32_load_row<D>(q, p.q + roff, half);
         f32_load_row<D>(dof, p.d_o + roff, half);
@@ -246,26 +256,26 @@ __global__ void __launch_bounds__(64 * kF32Waves, 1) hyd_cross_dq_fp32_kernel(Cr
             both_halves(Di, lo, hi);
             Di = lo + hi;
         }
-        if (split == 0 && half == 0 && i < rows) p.D[soff] = Di;
+        if (part == 0 && split == 0 && half == 0 && i < rows) p.D[soff] = Di;
         const float lse = p.lse_in[soff];
-        fl.load(rv, smem + kT, 0, stride_b);
+        fl.load(rk, smem, first, stride_b);
         f32x16 acc[NDB];
         f32_zero(acc);
-        for (int t = 0; t < n_kt; ++t) {
+        for (int t = t_lo; t < n_kt; ++t) {
             const uint32_t nxt = (uint32_t)(t + 1) * kF32Tile * stride_b;
             const bool more = t + 1 < n_kt;
-            if (t == max(n_kt - 2, 0)) wf.claim(p.hm, p.cursors);
+            if (t == max(n_kt - 2, t_lo)) wf.claim(p.hm, p.cursors);
             const int key0 = t * kF32Tile + 32 * split;
             const bool work = key0 < n && wrow0 < rows;
             f32x16 s[1], dp[1];
             f32_zero(s);
             f32_zero(dp);
-            if (t == 0) f32_arrive<kL>(); else f32_arrive<0>();  // K tile t (from the second tile on V was requested first)
-            if (work) f32_row_product(s[0], fl, 0, q);
-            if (t == 0) f32_arrive<0>();                         // V tile t
+            f32_arrive<kL>();                                       // V tile t is there; K was requested after it
             if (work) f32_row_product(dp[0], fl, kT, dof);
-            f32_release();
+            f32_wait_lds();
+            f32_arrive<0>();                                        // K tile t is there, V may be overwritten
             if (more) fl.load(rv, smem + kT, nxt, stride_b);
+            if (work) f32_row_product(s[0], fl, 0, q);
             if (work) {
                 const int rel = n - 1 - key0 - 4 * half;
 #pragma unroll
@@ -285,13 +295,14 @@ __global__ void __launch_bounds__(64 * kF32Waves, 1) hyd_cross_dq_fp32_kernel(Cr
         if (split == 0 && wrow0 < rows) {
 #pragma unroll
             for (int x = 1; x < kF32Splits; ++x) f32_add(acc, 1.f, smem + (2 * (x - 1) + rg) * kAcc, 1.f, lane);
-            if (i < rows) f32_store_row<D>(p.dq + roff, acc, p.scale, half);
+            if (i < rows) f32_store_row<D>(out + roff, acc, p.scale, half);
         }
     }
 }
 
-// dK/dV: 32 keys of a KV head, the query rows of its heads one after the other in tiles of 128 tokens.
-template <int D>
+// dK/dV: 32 keys of a KV head, the query rows of its heads one after the other in tiles of 128 tokens; kParts: parts of them.  (A
+// form of its own: the registers are full, and the parts' numbers cost the whole form 12 % at d = 128.)
+template <int D, bool kParts>
 __global__ void __launch_bounds__(64 * kF32KvWaves, 1) hyd_cross_dkdv_fp32_kernel(CrossF32Params p) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     constexpr int kT = f32_tile_bytes<D>(), NDB = D / 32;
@@ -307,15 +318,21 @@ __global__ void __launch_bounds__(64 * kF32KvWaves, 1) hyd_cross_dkdv_fp32_kerne
     WorkFetcher wf;
     WorkItem wi;
     for (bool have = wf.first(p.hm, p.hdr, p.cursors, p.items, slot, wi, blockIdx.x); have; have = wf.next(p.hm, p.cursors, p.items, slot, wi)) {
-        const int g = wi.head, keys = wi.lev, q0 = wi.row0 / G, L = wi.len / G;      // tokens of the sequence's queries
+        const int g = wi.head, keys = kParts ? wi.lev & ((1 << kCrossPartShift) - 1) : wi.lev, part = kParts ? wi.lev >> kCrossPartShift : 0;
+        const int q0 = wi.row0 / G, L = wi.len / G;              // tokens of the sequence's queries
         const int64_t koff = ((int64_t)(wi.seq + min(l32, keys - 1)) * p.c.hkv + g) * D;
-        const int n_iter = (L + kF32Tile - 1) / kF32Tile * G;
+        int it0 = 0, n_iter = (L + kF32Tile - 1) / kF32Tile * G;      // iterations: (tile, head), heads inner
+        if (kParts) {
+            const int per_part = (n_iter + p.parts - 1) / p.parts;
+            it0 = min(part * per_part, n_iter);
+            n_iter = min(it0 + per_part, n_iter) - it0;
+        }
         f32x16 acck[NDB], accv[NDB];
         f32_zero(acck);
         f32_zero(accv);
         if (n_iter == 0) wf.claim(p.hm, p.cursors);
         const uint32_t q_bytes = L > 0 ? (uint32_t)(L - 1) * stride_b + D * 4 : 0;
-        int ld_i = 0, ld_h = 0;
+        int ld_i = kParts ? it0 / G * kF32Tile : 0, ld_h = kParts ? it0 % G : 0;
         auto load_q = [&]() {
             fl.load(make_rsrc(p.q + ((int64_t)q0 * p.c.hq + g * G + ld_h) * D, q_bytes), smem, (uint32_t)ld_i * stride_b, stride_b);
         };
@@ -328,7 +345,7 @@ __global__ void __launch_bounds__(64 * kF32KvWaves, 1) hyd_cross_dkdv_fp32_kerne
         f32_load_row<D>(kr, p.k + koff, half);
         f32_load_row<D>(vr, p.v + koff, half);
         if (n_iter > 0) load_do();
-        int ti = 0, hh = 0;
+        int ti = kParts ? it0 / G * kF32Tile : 0, hh = kParts ? it0 % G : 0;
         for (int it = 0; it < n_iter; ++it) {
             const bool more = it + 1 < n_iter;
             if (it == max(n_iter - 2, 0)) wf.claim(p.hm, p.cursors);
@@ -386,8 +403,9 @@ __global__ void __launch_bounds__(64 * kF32KvWaves, 1) hyd_cross_dkdv_fp32_kerne
                 f32_add(accv, 1.f, smem + (2 * x + 1) * kAcc, 1.f, lane);
             }
             if (l32 < keys) {
-                f32_store_row<D>(p.dk + koff, acck, p.scale, half);
-                f32_store_row<D>(p.dv + koff, accv, 1.f, half);
+                const int64_t plane = (int64_t)p.c.Tk * p.c.hkv * D;
+                f32_store_row<D>((kParts ? p.part_o + part * plane : p.dk) + koff, acck, p.scale, half);
+                f32_store_row<D>((kParts ? p.part_o + (p.parts + part) * plane : p.dv) + koff, accv, 1.f, half);
             }
         }
     }

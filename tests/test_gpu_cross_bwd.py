@@ -102,6 +102,24 @@ def test_few_keys_and_few_rows_in_parts():
             c.bwd(o, lse, workspace=small[:-256])
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_few_items_in_parts_fp32(d):
+    """The same in fp32, with padded keys and a sequence without any."""
+    for lq, kv, hq, hkv, lens in (([9, 30, 2], [5000, 700, 40], 2, 1, [4777, 700, 0]), ([3000, 1, 2500], [30, 0, 70], 4, 2, [17, 0, 70])):
+        c = Case(lq, kv, hq, hkv, d, kv_lens=lens, seed=18, dtype="fp32", front=3, back=2)
+        o, lse = c.fwd()
+        outs = []
+        for fill in (0, 255):
+            ws = torch.full((64 << 20,), fill, dtype=torch.uint8, device="cuda")
+            dq, dk, dv = torch.full_like(c.q, 7.0), torch.full_like(c.k, 7.0), torch.full_like(c.v, 7.0)
+            c.bwd(o, lse, dq=dq, dk=dk, dv=dv, workspace=ws)
+            check_bwd(c, o, lse, dq, dk, dv)
+            for x, on in ((dq, c.q_rows), (dk, c.kv_rows), (dv, c.kv_rows)):
+                assert torch.all(x[torch.from_numpy(~on).cuda()] == 7.0)
+            outs.append((dq, dk, dv))
+        assert all(torch.equal(a, b) for a, b in zip(*outs))
+
+
 def test_list_with_many_sequences():
     rng = np.random.default_rng(8)
     for hq, hkv, d in ((8, 8, 64), (6, 3, 128)):
