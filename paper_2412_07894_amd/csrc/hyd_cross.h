@@ -169,35 +169,76 @@ __device__ __forceinline__ void store_packed_rows(AtFn at, int rows, const f32x1
     }
 }
 
-// ---- joining parts: each part of the keys has left O (fp32, divided by its own sum) and log2 of its sum, -inf where it saw none.
-// A group of D / 4 lanes takes a row; parts without keys are not read.
-constexpr int kCrossMaxParts = 64, kCrossJoinThreads = 256;
+// ---- joining parts: each part of the keys has left O (fp32, divided by its own sum) and log2 of its sum, -inf where it saw none
+// (such a part's O may be anything).  A group of D / 4 lanes adds parts of a row, four at a time; kWide: all groups of the
+// workgroup share the parts of one row.  Bound by latency: one token of 32 heads, d = 128, in 64 parts by single groups took 31 us.
+constexpr int kCrossMaxParts = 64, kCrossJoinThreads = 256, kCrossJoinFew = 4;
 struct CrossJoin {
     const float* part_o; const float* part_lse;      // [parts][Tq][Hq][d], [parts][Hq][Tq]
     void* o; float* lse;
     const int32_t* cu_q;
     int nseq, Tq, hq, parts;
 };
-template <int D, bool kF32>
+template <int D, bool kF32, bool kWide>
 __global__ void __launch_bounds__(kCrossJoinThreads) hyd_cross_join_kernel(CrossJoin p) {
-    constexpr int kLanes = D / 4, kRows = kCrossJoinThreads / kLanes;
-    const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / kLanes;
-    const int c = threadIdx.x % kLanes;
+    constexpr int kLanes = D / 4, kGroups = kCrossJoinThreads / kLanes;
+    const int grp = threadIdx.x / kLanes, c = threadIdx.x % kLanes;
+    const int64_t row = kWide ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * kGroups + grp;
     const int64_t rows = (int64_t)p.Tq * p.hq, plane = rows * D;
     if (row >= rows) return;
     const int t = (int)(row / p.hq), h = (int)(row - (int64_t)t * p.hq);
     if (t < p.cu_q[0] || t >= p.cu_q[p.nseq]) return;
     const float* pl = p.part_lse + (int64_t)h * p.Tq + t;
-    float m = -INFINITY;
-    for (int i = 0; i < p.parts; ++i) m = fmaxf(m, pl[i * rows]);
+    const float* po = p.part_o + row * D + 4 * c;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    float l = 0.f;
-    for (int i = 0; i < p.parts; ++i) {
-        const float x = pl[i * rows];
-        if (x == -INFINITY) continue;
-        const float w = __builtin_amdgcn_exp2f(x - m);
-        l += w;
-        sum += *reinterpret_cast<const f32x4*>(p.part_o + i * plane + row * D + 4 * c) * w;
+    float m = -INFINITY, l = 0.f;
+    const auto factor = [](float x, float top) { return x == top ? 1.f : __builtin_amdgcn_exp2f(x - top); };      // (both may be -inf)
+    constexpr int kStep = kWide ? kGroups : 1;
+    for (int i0 = kWide ? grp : 0; i0 < p.parts; i0 += 4 * kStep) {
+        float x[4], top = m;
+        f32x4 v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int i = min(i0 + u * kStep, p.parts - 1);
+            x[u] = pl[i * rows];
+            v[u] = *reinterpret_cast<const f32x4*>(po + i * plane);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (i0 + u * kStep >= p.parts) x[u] = -INFINITY;
+            top = fmaxf(top, x[u]);
+        }
+        const float f = factor(m, top);
+        sum *= f;
+        l *= f;
+        m = top;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (x[u] == -INFINITY) continue;
+            const float w = __builtin_amdgcn_exp2f(x[u] - m);
+            l += w;
+            sum += v[u] * w;
+        }
+    }
+    if (kWide) {
+        __shared__ f32x4 sums[kCrossJoinThreads];
+        __shared__ float ml[2][kGroups];
+        sums[threadIdx.x] = sum;
+        if (c == 0) { ml[0][grp] = m; ml[1][grp] = l; }
+        __syncthreads();
+        if (grp) return;
+        float top = -INFINITY;
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) top = fmaxf(top, ml[0][g]);
+        sum = f32x4{0.f, 0.f, 0.f, 0.f};
+        l = 0.f;
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            const float f = factor(ml[0][g], top);
+            l += ml[1][g] * f;
+            sum += sums[g * kLanes + c] * f;
+        }
+        m = top;
     }
     const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);      // (a NaN stays one)
     sum *= inv;

@@ -160,11 +160,12 @@ CrossShape shape_of(const Sizes& z, const int32_t* cu_q, const int32_t* cu_kv, c
     return c;
 }
 
-template <int D>
-void launch_join(const CrossJoin& j, bool f32, hipStream_t st) {
-    constexpr int kRows = kCrossJoinThreads / (D / 4);
+template <int D, bool kF32>
+void launch_join(const CrossJoin& j, hipStream_t st) {
     KernelTimer kt("cross_join", st);
-    hipLaunchKernelGGL((f32 ? hyd_cross_join_kernel<D, true> : hyd_cross_join_kernel<D, false>), dim3((unsigned)tiles((long long)j.Tq * j.hq, kRows)), dim3(kCrossJoinThreads), 0, st, j);
+    const long long rows = (long long)j.Tq * j.hq;
+    if (j.parts > kCrossJoinFew) hipLaunchKernelGGL((hyd_cross_join_kernel<D, kF32, true>), dim3((unsigned)rows), dim3(kCrossJoinThreads), 0, st, j);
+    else hipLaunchKernelGGL((hyd_cross_join_kernel<D, kF32, false>), dim3((unsigned)tiles(rows, kCrossJoinThreads / (D / 4))), dim3(kCrossJoinThreads), 0, st, j);
 }
 
 template <int D>
@@ -183,11 +184,16 @@ void launch_fwd(const Sizes& z, const CrossShape& c, const void* q, const void* 
         p.o = static_cast<uint16_t*>(o); p.lse = lse; p.scale_log2 = scale * kLog2eHost;
         const long long items = (long long)z.nseq * z.hkv;
         constexpr int kTurn = kFewWaves * kFewKeys;
+        // Parts of the keys: one item for a CU or, if there are more, 8, whose ends then hardly differ; each of two turns of the waves at
+        // least (four where the chip is full).  Up to four turns the keys stay whole: a second launch costs 3 us (4 tokens of 32/8
+        // heads, d = 128, whole and in parts: 700 keys 9.4 and 11.0 us, 1500 keys 12.7 and 10.9, 8000 keys 52 and 26).
         long long want = items >= kCus ? tiles(8 * kCus, items) : kCus / items;
         if (want > kCrossMaxParts) want = kCrossMaxParts;
         long long chunk = tiles(tiles(z.max_kv, want), kTurn) * kTurn;
-        if (items >= kCus && chunk < 4 * kTurn) chunk = 4 * kTurn;
-        j.parts = parts_in_room(w, z, ws_bytes, (int)tiles(z.max_kv, chunk));
+        const long long least = items >= kCus ? 4 * kTurn : 2 * kTurn;
+        if (chunk < least) chunk = least;
+        if (z.max_kv <= 4 * kTurn) chunk = z.max_kv;
+        j.parts = z.max_kv > 0 ? parts_in_room(w, z, ws_bytes, (int)tiles(z.max_kv, chunk)) : 1;
         p.parts = j.parts;
         p.chunk = j.parts == 1 ? z.max_kv : (int)(tiles(tiles(z.max_kv, j.parts), kTurn) * kTurn);
         p.part_o = const_cast<float*>(j.part_o); p.part_lse = part_lse(j.parts);
@@ -235,7 +241,8 @@ void launch_fwd(const Sizes& z, const CrossShape& c, const void* q, const void* 
     }
     if (j.parts > 1) {
         j.part_lse = part_lse(j.parts);
-        launch_join<D>(j, z.dt == HYD_FP32, st);
+        if (z.dt == HYD_FP32) launch_join<D, true>(j, st);
+        else launch_join<D, false>(j, st);
     }
 }
 
