@@ -81,7 +81,7 @@ int parts_in_room(const FwdLayout& w, const Sizes& z, size_t bytes, int want) {
 }
 
 // ---- backward
-constexpr int kBwdMaxParts = 16, kDqPartRows = 65536, kKvPartRows = 131072, kBwdItems = 512;
+constexpr int kBwdMaxParts = 16, kDqPartRows = 65536, kKvPartRows = 131072, kBwdItems = 2 * kCus;
 struct BwdLayout { size_t q_hdr, q_items, kv_hdr, kv_items, stat[4], q16, do16, k16, absmax, need, total; long long n_q, n_kv; };
 BwdLayout bwd_layout(const Sizes& z) {
     BwdLayout w;
@@ -89,7 +89,7 @@ BwdLayout bwd_layout(const Sizes& z) {
     w.n_q = most_tiles((long long)z.Tq * G, (long long)z.max_q * G, z.nseq, tile_q(z.dt));
     w.n_kv = most_tiles(z.Tk, z.max_kv, z.nseq, tile_kv(z.dt));
     const size_t q_elems = (size_t)z.Tq * z.hq * z.d, kv_elems = (size_t)z.Tk * z.hkv * z.d;
-    const auto records = [](long long n) { return align_up(16 * (size_t)(n > kCus ? n : kCus)); };      // (in parts: kCus records at most)
+    const auto records = [](long long n) { return align_up(16 * (size_t)(n > kBwdItems ? n : kBwdItems)); };      // (in parts: kBwdItems records at most)
     size_t at = 0;
     w.q_hdr = at;    at += align_up(sizeof(int) * kHdrTotal);
     w.q_items = at;  at += records(w.n_q);

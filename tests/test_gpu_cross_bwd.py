@@ -102,6 +102,11 @@ def test_few_keys_and_few_rows_in_parts():
             c.bwd(o, lse, workspace=small[:-256])
 
 
+def test_many_key_tiles_in_parts():
+    """Two parts of 200 key tiles: more records of key tiles than CUs."""
+    both(Case([1100], [200 * 256 - 5], 1, 1, 64, seed=28))
+
+
 @pytest.mark.parametrize("d", [64, 128])
 def test_few_items_in_parts_fp32(d):
     """The same in fp32, with padded keys and a sequence without any."""
