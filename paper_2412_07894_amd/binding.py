@@ -314,16 +314,25 @@ def cross_attn_workspace_bytes(total_q, total_kv, num_seqs, max_seqlen_q, max_se
                                                      dtype_code, int(bool(is_bwd))))
 
 
-def _like(name, t, shape, dtype, device):
-    """t as it is, checked; made if None."""
-    if t is None:
+def _made(shape, dtype, device, stream):
+    """A new tensor that belongs to the stream its kernel runs on: its memory may have been another tensor's of that stream, but of no
+    other stream that still works on it."""
+    if stream is None:
         return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _like(name, t, shape, dtype, device, stream=None):
+    """t as it is, checked; made for `stream` if None."""
+    if t is None:
+        return _made(shape, dtype, device, stream)
     if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {tuple(shape)} tensor of {dtype} on {device}, got {tuple(t.shape)} {t.dtype} {t.device}")
     return t
 
 
-def _cross_sizes(q, k, v, cu_q, cu_kv, max_seqlen_q, max_seqlen_kv, workspace, is_bwd):
+def _cross_sizes(q, k, v, cu_q, cu_kv, max_seqlen_q, max_seqlen_kv, workspace, is_bwd, stream):
     """Checks of the tensors that both directions take: (Tq, Tk, num_seqs, Hq, Hkv, d, dtype code, workspace)."""
     if q.dim() != 3 or k.dim() != 3:
         raise ValueError(f"q and k must be [rows, heads, d], got {tuple(q.shape)} and {tuple(k.shape)}")
@@ -337,7 +346,8 @@ def _cross_sizes(q, k, v, cu_q, cu_kv, max_seqlen_q, max_seqlen_kv, workspace, i
     if nseq < 0 or cu_kv.numel() != nseq + 1:
         raise ValueError(f"cu_q and cu_kv must have num_seqs + 1 elements, got {cu_q.numel()} and {cu_kv.numel()}")
     if workspace is None:
-        workspace = _workspace(cross_attn_workspace_bytes(Tq, Tk, nseq, max_seqlen_q, max_seqlen_kv, hq, hkv, d, dt, is_bwd), dev)
+        nbytes = cross_attn_workspace_bytes(Tq, Tk, nseq, max_seqlen_q, max_seqlen_kv, hq, hkv, d, dt, is_bwd)
+        workspace = _made(max(nbytes, 256), torch.uint8, dev, stream)
     elif workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.device != dev:
         raise ValueError(f"workspace must be a contiguous uint8 tensor on {dev}, got {workspace.dtype} {workspace.device}")
     return Tq, Tk, nseq, hq, hkv, d, dt, workspace
@@ -353,11 +363,12 @@ def cross_attn_fwd(q, k, v, cu_q, cu_kv, max_seqlen_q, max_seqlen_kv, softmax_sc
                    workspace=None, stream=None, out=None, lse=None):
     """Cross attention of packed batches: queries q[Tq,Hq,d] of sequence s (rows cu_q[s]..cu_q[s+1]) on all its keys in k, v[Tk,Hkv,d]
     (rows cu_kv[s]..cu_kv[s+1], of which kv_lens[s] are valid, all if kv_lens is None).  Returns (o[Tq,Hq,d], lse[Hq,Tq] fp32);
-    a sequence without valid keys gets o = 0, lse = -inf.  Work goes to `stream`, by default the current one of q's device."""
-    Tq, Tk, nseq, hq, hkv, d, dt, ws = _cross_sizes(q, k, v, cu_q, cu_kv, max_seqlen_q, max_seqlen_kv, workspace, False)
+    a sequence without valid keys gets o = 0, lse = -inf.  Work goes to `stream`, by default the current one of q's device; so do the
+    tensors that are made here."""
+    Tq, Tk, nseq, hq, hkv, d, dt, ws = _cross_sizes(q, k, v, cu_q, cu_kv, max_seqlen_q, max_seqlen_kv, workspace, False, stream)
     dev = q.device
-    o = _like("out", out, q.shape, q.dtype, dev)
-    lse = _like("lse", lse, (hq, Tq), torch.float32, dev)
+    o = _like("out", out, q.shape, q.dtype, dev, stream)
+    lse = _like("lse", lse, (hq, Tq), torch.float32, dev, stream)
     kq, hp_q = _host_lens("cu_q_host", cu_q_host, nseq)
     kk, hp_k = _host_lens("cu_kv_host", cu_kv_host, nseq)
     _on_device(dev, load().hyd_cross_attn_fwd,
@@ -371,14 +382,14 @@ def cross_attn_bwd(q, k, v, o, lse, d_o, cu_q, cu_kv, max_seqlen_q, max_seqlen_k
                    cu_kv_host=None, workspace=None, stream=None, dq=None, dk=None, dv=None):
     """Gradients (dq, dk, dv) of cross_attn_fwd for an upstream gradient d_o of o; o and lse are the forward's results.  Rows of dk
     and dv behind a sequence's valid keys are zeros."""
-    Tq, Tk, nseq, hq, hkv, d, dt, ws = _cross_sizes(q, k, v, cu_q, cu_kv, max_seqlen_q, max_seqlen_kv, workspace, True)
+    Tq, Tk, nseq, hq, hkv, d, dt, ws = _cross_sizes(q, k, v, cu_q, cu_kv, max_seqlen_q, max_seqlen_kv, workspace, True, stream)
     dev = q.device
     _like("o", o, q.shape, q.dtype, dev)
     _like("d_o", d_o, q.shape, q.dtype, dev)
     _like("lse", lse, (hq, Tq), torch.float32, dev)
-    dq = _like("dq", dq, q.shape, q.dtype, dev)
-    dk = _like("dk", dk, k.shape, k.dtype, dev)
-    dv = _like("dv", dv, v.shape, v.dtype, dev)
+    dq = _like("dq", dq, q.shape, q.dtype, dev, stream)
+    dk = _like("dk", dk, k.shape, k.dtype, dev, stream)
+    dv = _like("dv", dv, v.shape, v.dtype, dev, stream)
     kq, hp_q = _host_lens("cu_q_host", cu_q_host, nseq)
     kk, hp_k = _host_lens("cu_kv_host", cu_kv_host, nseq)
     _on_device(dev, load().hyd_cross_attn_bwd,
@@ -400,14 +411,14 @@ def rope_frequencies(rot_dim, base=10000.0, scaling="plain", factor=1.0, origina
     return torch.from_numpy(out).to(device)
 
 
-def _rope_tensor(name, x, out, T, d, dt, device):
+def _rope_tensor(name, x, out, T, d, dt, device, stream):
     """Checks a tensor of rope_rotate and its output (made if None), [T, heads, d] with the heads of a token contiguous: (output,
     heads, the tensor's token stride, the output's)."""
     shape = x.shape
     if len(shape) != 3 or shape[0] != T or shape[2] != d or x.dtype != dt or x.device != device:
         raise ValueError(f"{name} must be [{T}, heads, {d}] in {dt} on {device}, got {tuple(shape)} {x.dtype} {x.device}")
     if out is None:
-        out = torch.empty(shape, dtype=dt, device=device)
+        out = _made(shape, dt, device, stream)
     elif out.shape != shape or out.dtype != dt or out.device != device:
         raise ValueError(f"the output of {name} must be like it, got {tuple(out.shape)} {out.dtype} {out.device}")
     heads = shape[1]
@@ -434,7 +445,7 @@ def rope_rotate(q, freqs, k=None, cu_seqlens=None, starts=None, positions=None, 
     """Rotary positions on q[T,H,d] and, with k[T,Hk,d], on both in one launch (bf16 or fp32, the rows may be strided); the first
     2 * freqs.numel() elements of every head are turned.  The rows' positions are `positions` (int32 [T]) or follow from
     cu_seqlens (int32 [num_seqs+1]) and `starts` (int32 [num_seqs] or None).  out may be q, k_out may be k.  Returns out, or
-    (out, k_out).  Work goes to `stream`, by default the current one of q's device."""
+    (out, k_out).  Work goes to `stream`, by default the current one of q's device; so do the tensors that are made here."""
     if q.dim() != 3:
         raise ValueError(f"q must be [T, heads, d], got {tuple(q.shape)}")
     T, hq, d = q.shape
@@ -450,10 +461,10 @@ def rope_rotate(q, freqs, k=None, cu_seqlens=None, starts=None, positions=None, 
     nseq = 0 if cu_seqlens is None else cu_seqlens.numel() - 1
     if nseq < 0:
         raise ValueError("cu_seqlens must have num_seqs + 1 elements")
-    out, hq, qs, qos = _rope_tensor("q", q, out, T, d, q.dtype, dev)
+    out, hq, qs, qos = _rope_tensor("q", q, out, T, d, q.dtype, dev, stream)
     kp, kop, hk, ks, kos = None, None, 0, 0, 0
     if k is not None:
-        k_out, hk, ks, kos = _rope_tensor("k", k, k_out, T, d, q.dtype, dev)
+        k_out, hk, ks, kos = _rope_tensor("k", k, k_out, T, d, q.dtype, dev, stream)
         kp, kop = k.data_ptr(), k_out.data_ptr()
     _on_device(dev, load().hyd_rope_rotate,
                (q.data_ptr(), hq, qs, out.data_ptr(), qos, kp, hk, ks, kop, kos, _int32("cu_seqlens", cu_seqlens, nseq + 1, dev),

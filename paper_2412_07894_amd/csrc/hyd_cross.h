@@ -86,7 +86,7 @@ __device__ __forceinline__ void cross_build_list(const CrossShape& c, const Cros
         const auto put = [&](int f, int m, int o0, int o, int a, int i) {
             const int tile = i / l.parts, part = i - tile * l.parts;
             const i32x4 rec = {f + tile * l.tile, min(m - tile * l.tile, l.tile) | (part << kCrossPartShift), o0, o};
-            if (a + i < l.max_items) *reinterpret_cast<i32x4*>(l.items + 4 * (size_t)(a + i)) = rec;
+            if ((unsigned)(a + i) < (unsigned)l.max_items) *reinterpret_cast<i32x4*>(l.items + 4 * (size_t)(a + i)) = rec;
         };
         constexpr int kFew = 4;           // sequences of more items: by the whole wave
         if (count <= kFew)

@@ -89,8 +89,8 @@ __global__ void __launch_bounds__(kKeysThreads, 1) hyd_cross_bwd_keys_bf16_kerne
     CrossRows cr;
     cr.init(G);
     if (part == 0)                                        // behind the valid keys: zeros
-        for (int i = n * (D / 8) + tid; i < x.rows * (D / 8); i += kKeysThreads) {
-            const int64_t at = kv_at + (int64_t)(i / (D / 8)) * kv_stride + 8 * (i % (D / 8));
+        for (int64_t i = n * (D / 8) + tid; i < (int64_t)x.rows * (D / 8); i += kKeysThreads) {
+            const int64_t at = kv_at + i / (D / 8) * kv_stride + 8 * (i % (D / 8));
             *reinterpret_cast<u32x4*>(p.dk + at) = u32x4{0u, 0u, 0u, 0u};
             *reinterpret_cast<u32x4*>(p.dv + at) = u32x4{0u, 0u, 0u, 0u};
         }
