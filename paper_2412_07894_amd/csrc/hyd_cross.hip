@@ -184,15 +184,16 @@ void launch_fwd(const Sizes& z, const CrossShape& c, const void* q, const void* 
         p.o = static_cast<uint16_t*>(o); p.lse = lse; p.scale_log2 = scale * kLog2eHost;
         const long long items = (long long)z.nseq * z.hkv;
         constexpr int kTurn = kFewWaves * kFewKeys;
-        // Parts of the keys: one item for a CU or, if there are more, 8, whose ends then hardly differ; each of two turns of the waves at
-        // least (four where the chip is full).  Up to four turns the keys stay whole: a second launch costs 3 us (4 tokens of 32/8
-        // heads, d = 128, whole and in parts: 700 keys 9.4 and 11.0 us, 1500 keys 12.7 and 10.9, 8000 keys 52 and 26).
-        long long want = items >= kCus ? tiles(8 * kCus, items) : kCus / items;
+        // Parts of the keys: two workgroups for a CU, or if there are as many items as CUs, 32, whose ends then hardly differ;
+        // each of 512 keys at least (1024 where the chip is full).  Up to 1024 keys (2048) they stay whole: a second launch costs 3 us.
+        // Whole and in parts: 4 tokens of 32/8 heads, d = 128, 700 keys 9.4 and 11.0 us, 1500 keys 12.7 and 10.9, 8000 keys 52 and 26;
+        // 40 tokens of 8 heads, d = 64, 1 to 30000 keys 462 and 293 us.
+        long long want = items >= kCus ? tiles(32 * kCus, items) : 2 * kCus / items;
         if (want > kCrossMaxParts) want = kCrossMaxParts;
         long long chunk = tiles(tiles(z.max_kv, want), kTurn) * kTurn;
-        const long long least = items >= kCus ? 4 * kTurn : 2 * kTurn;
+        const long long least = (items >= kCus ? 8 : 4) * kTurn;
         if (chunk < least) chunk = least;
-        if (z.max_kv <= 4 * kTurn) chunk = z.max_kv;
+        if (z.max_kv <= 2 * least) chunk = z.max_kv;
         j.parts = z.max_kv > 0 ? parts_in_room(w, z, ws_bytes, (int)tiles(z.max_kv, chunk)) : 1;
         p.parts = j.parts;
         p.chunk = j.parts == 1 ? z.max_kv : (int)(tiles(tiles(z.max_kv, j.parts), kTurn) * kTurn);

@@ -205,12 +205,14 @@ __global__ void __launch_bounds__(kFwdThreads, 1) hyd_cross_fwd_bf16_kernel(Cros
 // ---------------------------------------------------------------------------------------------
 // Few rows: at most 32 packed rows of a (sequence, KV head), as when a model writes one token after the other.  Bound by HBM: K and V
 // are read once and 32 rows cost the matrix pipe the same as one.  So the keys are spread: over workgroups in parts of `chunk` keys,
-// inside one over its 8 waves in turns of 32 keys, and each wave streams its own keys through its own 16 KB of LDS (K and V, 32
+// inside one over its 4 waves in turns of 32 keys, and each wave streams its own keys through its own 16 KB of LDS (K and V, 32
 // rows each) without meeting the others: K of its next turn is requested as soon as the scores are formed, V as soon as
 // the second product is done, so that 64 to 128 KB are under way per CU.  The waves' results meet in LDS once, the parts' by
-// hyd_cross_join_kernel.
+// hyd_cross_join_kernel.  Two workgroups share a CU, so that one streams while the other begins or ends: with one of 8 waves 64 tokens
+// of 32/8 heads, d = 128, against 500 to 8192 keys took 258 us, so 222 (1.13 GB, 5.1 TB/s); 16 against 30000 keys 380 us
+// (5.2 TB/s); the smallest calls, 11 us, are two launches.
 // ---------------------------------------------------------------------------------------------
-constexpr int kFewRows = 32, kFewKeys = 32, kFewWaves = 8, kFewThreads = 64 * kFewWaves;
+constexpr int kFewRows = 32, kFewKeys = 32, kFewWaves = 4, kFewThreads = 64 * kFewWaves;
 constexpr int kFewTileBytes = kFewKeys * kRowBytes;                   // 8 KB
 constexpr int kFewWaveBytes = 2 * kFewTileBytes;                      // K, V; later the wave's sums
 constexpr int kFewMlOff = kFewWaves * kFewWaveBytes;                  // [wave][m, l][32 rows]
@@ -225,7 +227,7 @@ struct CrossFewParams {
 };
 
 template <int D>
-__global__ void __launch_bounds__(kFewThreads, 1) hyd_cross_few_bf16_kernel(CrossFewParams p) {
+__global__ void __launch_bounds__(kFewThreads, 2) hyd_cross_few_bf16_kernel(CrossFewParams p) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
     constexpr int kRowB = D * 2, NK = D / 16, NDB = D / 32;
@@ -262,7 +264,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) hyd_cross_few_bf16_kernel(Cros
     const float scale_log2 = fmaxf(fabsf(p.scale_log2), 1e-30f);
     const uint32_t sign_flip = p.scale_log2 < 0.f ? 0x80008000u : 0u;
 
-    // keys of this wave's turn t: first + (8 t + wave) * 32 + 0..31; reads past `last` return zero
+    // keys of this wave's turn t: first + (4 t + wave) * 32 + 0..31; reads past `last` return zero
     const int n_turns = max((last - first - wave * kFewKeys + kFewWaves * kFewKeys - 1) / (kFewWaves * kFewKeys), 0);
     const uint32_t kv_bytes = last > first ? (uint32_t)(last - first - 1) * kv_stride_b + kRowB : 0;
     const int64_t kv_off = (int64_t)(x.k0 + first) * kv_stride + (int64_t)g * D;
