@@ -171,7 +171,7 @@ __device__ __forceinline__ void store_packed_rows(AtFn at, int rows, const f32x1
 
 // ---- joining parts: each part of the keys has left O (fp32, divided by its own sum) and log2 of its sum, -inf where it saw none
 // (such a part's O may be anything).  A group of D / 4 lanes adds parts of a row, four at a time; kWide: all groups of the
-// workgroup share the parts of one row.  Bound by latency: one token of 32 heads, d = 128, in 64 parts by single groups took 31 us.
+// workgroup share the parts of one row.  Bound by latency: 2 us and the launch; one token of 32 heads, d = 128, in 64 parts by single groups took 31 us.
 constexpr int kCrossMaxParts = 64, kCrossJoinThreads = 256, kCrossJoinFew = 4;
 struct CrossJoin {
     const float* part_o; const float* part_lse;      // [parts][Tq][Hq][d], [parts][Hq][Tq]

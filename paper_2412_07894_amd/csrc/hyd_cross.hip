@@ -111,7 +111,8 @@ BwdLayout bwd_layout(const Sizes& z) {
     return w;
 }
 // Parts of an item where `items` of them leave workgroups idle: up to `target` in all, none shorter than `least` of its `steps`, and as
-// many as their sums of `row_bytes` have room for (most_rows of `rows` at most).
+// many as their sums of `row_bytes` have room for (most_rows of `rows` at most).  Whole and in parts: 50 queries against 2000 keys, fp32,
+// d = 128, dQ 220 and 55 us; 4000 against 77 keys, dK/dV 350 and 66 us.
 int bwd_parts(long long items, int target, long long steps, int least, size_t rows, size_t most_rows, size_t row_bytes, size_t room) {
     long long n = items > 0 ? target / items : 1;
     if (n > steps / least) n = steps / least;
@@ -202,6 +203,7 @@ void launch_fwd(const Sizes& z, const CrossShape& c, const void* q, const void* 
         hipLaunchKernelGGL(hyd_cross_few_bf16_kernel<D>, dim3((unsigned)(items * p.parts)), dim3(kFewThreads), kFewLds, st, p);
     } else {
         // items of whole tiles: own ones where they all fit on the chip, with the keys in parts where they do not fill it, else from a list
+        // (2 x 200 queries of 8/2 heads against 8000 keys, d = 128: 16 parts 34 us, whole 179 us)
         const int tile = tile_q(z.dt), key_tile = z.dt == HYD_BF16 ? kFwdBN : kF32Tile;
         const long long per_seq = tiles(rows, tile), own = (long long)z.nseq * per_seq * z.hkv;
         const bool self = own <= kCus;
