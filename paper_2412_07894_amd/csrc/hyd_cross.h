@@ -31,6 +31,26 @@ __device__ __forceinline__ CrossSeq cross_seq(const CrossShape& c, int s) {
     return x;
 }
 
+// ---- zeros behind the valid keys, by n workgroups of which so many share a sequence
+struct CrossZero { int n, per_seq; };
+inline CrossZero cross_zero(int nseq, bool padded) {
+    constexpr int kZeroWg = 256;
+    if (!padded) return CrossZero{0, 1};
+    return nseq < kZeroWg ? CrossZero{kZeroWg / nseq * nseq, kZeroWg / nseq} : CrossZero{kZeroWg, 1};
+}
+// E: 16 bytes of an element type, kPer elements; row: elements of a key row
+template <typename E, int kPer, typename T>
+__device__ __forceinline__ void cross_clear(const CrossShape& c, const CrossZero& z, int wg, int nthreads, int64_t row, T* dk, T* dv) {
+    for (int s = wg / z.per_seq; s < c.nseq; s += z.n / z.per_seq) {
+        const CrossSeq x = cross_seq(c, s);
+        const int64_t last = (int64_t)(x.k0 + x.rows) * row / kPer;
+        for (int64_t i = (int64_t)(x.k0 + x.n) * row / kPer + (wg % z.per_seq) * nthreads + threadIdx.x; i < last; i += (int64_t)z.per_seq * nthreads) {
+            *reinterpret_cast<E*>(dk + kPer * i) = E{};
+            *reinterpret_cast<E*>(dv + kPer * i) = E{};
+        }
+    }
+}
+
 // ---- item lists (WorkFetcher hands them out).  A record names a tile by rows, so that nothing has to be looked up:
 //   queries: {first packed row (over all sequences), rows | part << 16, first key row, keys}
 //   keys:    {first key row, keys | part << 16, first packed row, packed rows}

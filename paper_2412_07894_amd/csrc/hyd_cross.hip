@@ -297,13 +297,13 @@ void launch_bwd(const Sizes& z, const CrossShape& c, const BwdArgs& a, float sca
         p.tok = prep_tokens(z.Tq, z.hq);
         p.n_q = sc.n_absmax = prep_workgroups(z.Tq, p.tok);
         p.sc = sc;
-        p.n_zero = !c.kv_lens ? 0 : (z.nseq < kCus ? z.nseq : kCus);
+        p.zero = cross_zero(z.nseq, c.kv_lens != nullptr);
         const long long copies = tiles((long long)z.Tk * z.hkv, 4 * kPrepThreads / (D / 8));
         const int n_k = (int)(copies < kPrepTarget ? copies : kPrepTarget);
         p.lists[0] = CrossList{q_hdr, q_items, kDqBM, parts_q, (int)(w.n_q * parts_q), false};
         p.lists[1] = CrossList{kv_hdr, kv_items, kKwBN, parts_kv, (int)(w.n_kv * parts_kv), true};
         KernelTimer kt("cross_prep", st);
-        hipLaunchKernelGGL(hyd_cross_prep_bf16_kernel<D>, dim3((unsigned)(kCrossLists + p.n_zero + p.n_q + n_k)), dim3(kPrepThreads), cross_prep_lds(z.hq, p.tok), st, p);
+        hipLaunchKernelGGL(hyd_cross_prep_bf16_kernel<D>, dim3((unsigned)(kCrossLists + p.zero.n + p.n_q + n_k)), dim3(kPrepThreads), cross_prep_lds(z.hq, p.tok), st, p);
     }
     const auto grid_of = [&](long long work) { return (int)(work < 1 ? 1 : (work < cus ? work : cus)); };
     {
@@ -351,9 +351,9 @@ void launch_bwd_f32(const Sizes& z, const CrossShape& c, const BwdArgs& a, float
         b.c = c; b.dk = static_cast<float*>(a.dk); b.dv = static_cast<float*>(a.dv); b.d = D;
         b.lists[0] = CrossList{hdr[0], items[0], kF32BM, parts_q, (int)(w.n_q * parts_q), false};
         b.lists[1] = CrossList{hdr[1], items[1], kF32KvBN, parts_kv, (int)(w.n_kv * parts_kv), true};
-        const int n_zero = !c.kv_lens ? 0 : (z.nseq < kCus ? z.nseq : kCus);
+        b.zero = cross_zero(z.nseq, c.kv_lens != nullptr);
         KernelTimer kt("cross_begin", st);
-        hipLaunchKernelGGL(hyd_cross_begin_fp32_kernel, dim3(2 + n_zero), dim3(kPreludeThreads), kCrossListLds, st, b);
+        hipLaunchKernelGGL(hyd_cross_begin_fp32_kernel, dim3(2 + b.zero.n), dim3(kPreludeThreads), kCrossListLds, st, b);
     }
     CrossF32Params p;
     memset(&p, 0, sizeof(p));

@@ -12,7 +12,7 @@
 namespace hyd {
 
 // ---------------------------------------------------------------------------------------------
-// Preparation, one launch: workgroups 0 and 1 build the item lists, then n_zero of them clear dK and dV behind the valid keys of
+// Preparation, one launch: workgroups 0 and 1 build the item lists, then zero.n of them clear dK and dV behind the valid keys of
 // their sequences (padded caches), n_q make one pass over O and dO (row statistics, negated, and the maxima of |dO|), the others
 // copy K to fp16.  Bound by HBM, or by latency on small batches: 24 sequences, 18000 keys and 5400 queries of 20 heads, d = 64, 120 MB, 28 us.
 // ---------------------------------------------------------------------------------------------
@@ -22,7 +22,8 @@ struct CrossPrepParams {
     uint16_t* dk; uint16_t* dv;
     BwdScratch sc;
     int tok;                              // tokens of a statistics workgroup at a time
-    int n_zero, n_q;                      // workgroups
+    CrossZero zero;
+    int n_q;                              // workgroups of the pass over O and dO
     CrossList lists[2];
 };
 constexpr int kCrossLists = 2;
@@ -43,22 +44,15 @@ __global__ void __launch_bounds__(kPrepThreads) hyd_cross_prep_bf16_kernel(Cross
     wg -= kCrossLists;
     constexpr int kLanes = D / 8, kGrps = kPrepThreads / kLanes, kU = 4;      // lanes per row, rows at a time, in flight
     const int hq = p.c.hq, hkv = p.c.hkv, G = p.c.G, tok = p.tok;
-    if (wg < p.n_zero) {
-        for (int s = wg; s < p.c.nseq; s += p.n_zero) {
-            const CrossSeq x = cross_seq(p.c, s);
-            const int64_t first = (int64_t)(x.k0 + x.n) * hkv * kLanes, last = (int64_t)(x.k0 + x.rows) * hkv * kLanes;
-            for (int64_t i = first + tid; i < last; i += kPrepThreads) {
-                *reinterpret_cast<u32x4*>(p.dk + 8 * i) = u32x4{0u, 0u, 0u, 0u};
-                *reinterpret_cast<u32x4*>(p.dv + 8 * i) = u32x4{0u, 0u, 0u, 0u};
-            }
-        }
+    if (wg < p.zero.n) {
+        cross_clear<u32x4, 8>(p.c, p.zero, wg, kPrepThreads, (int64_t)hkv * D, p.dk, p.dv);
         return;
     }
-    wg -= p.n_zero;
+    wg -= p.zero.n;
     const int grp = tid / kLanes, c = tid % kLanes;
     if (wg >= p.n_q) {                             // fp16 copy of K, rows [cu_kv[0], cu_kv[nseq])
         const int64_t first = (int64_t)max(p.c.cu_kv[0], 0) * hkv, last = (int64_t)min(p.c.cu_kv[p.c.nseq], p.c.Tk) * hkv;
-        const int64_t step = (int64_t)(gridDim.x - kCrossLists - p.n_zero - p.n_q) * kGrps * kU;
+        const int64_t step = (int64_t)(gridDim.x - kCrossLists - p.zero.n - p.n_q) * kGrps * kU;
         for (int64_t r0 = first + (int64_t)(wg - p.n_q) * kGrps * kU + grp; r0 < last; r0 += step) {
             u32x4 x[kU];
 #pragma unroll

@@ -26,21 +26,14 @@ struct CrossF32Params {
 };
 
 // Item lists of the backward (workgroups 0 and 1), zeros in dK and dV behind the valid keys (the others).
-struct CrossF32Begin { CrossShape c; CrossList lists[2]; float* dk; float* dv; int d; };
+struct CrossF32Begin { CrossShape c; CrossList lists[2]; CrossZero zero; float* dk; float* dv; int d; };
 __global__ void __launch_bounds__(kPreludeThreads) hyd_cross_begin_fp32_kernel(CrossF32Begin p) {
     extern __shared__ int lds_classes[];
     if (blockIdx.x < 2) {
         cross_build_list(p.c, p.lists[blockIdx.x], lds_classes, kPreludeThreads);
         return;
     }
-    for (int s = (int)blockIdx.x - 2; s < p.c.nseq; s += (int)gridDim.x - 2) {
-        const CrossSeq x = cross_seq(p.c, s);
-        const int64_t row = (int64_t)p.c.hkv * p.d / 4, first = (x.k0 + x.n) * row, last = (x.k0 + x.rows) * row;
-        for (int64_t i = first + threadIdx.x; i < last; i += kPreludeThreads) {
-            *reinterpret_cast<f32x4*>(p.dk + 4 * i) = f32x4{0.f, 0.f, 0.f, 0.f};
-            *reinterpret_cast<f32x4*>(p.dv + 4 * i) = f32x4{0.f, 0.f, 0.f, 0.f};
-        }
-    }
+    cross_clear<f32x4, 4>(p.c, p.zero, (int)blockIdx.x - 2, kPreludeThreads, (int64_t)p.c.hkv * p.d, p.dk, p.dv);
 }
 
 // LDS reads of this wave done (before a barrier after which the tile may be overwritten)

@@ -91,12 +91,12 @@ __global__ void __launch_bounds__(kKeysThreads, 1) hyd_cross_bwd_keys_bf16_kerne
     const int64_t kv_at = (int64_t)x.k0 * kv_stride + (int64_t)g * D;
     CrossRows cr;
     cr.init(G);
-    if (part == 0)                                        // behind the valid keys: zeros
-        for (int64_t i = n * (D / 8) + tid; i < (int64_t)x.rows * (D / 8); i += kKeysThreads) {
-            const int64_t at = kv_at + i / (D / 8) * kv_stride + 8 * (i % (D / 8));
-            *reinterpret_cast<u32x4*>(p.dk + at) = u32x4{0u, 0u, 0u, 0u};
-            *reinterpret_cast<u32x4*>(p.dv + at) = u32x4{0u, 0u, 0u, 0u};
-        }
+    // behind the valid keys: zeros
+    for (int64_t i = n * (D / 8) + part * kKeysThreads + tid; i < (int64_t)x.rows * (D / 8); i += (int64_t)p.parts * kKeysThreads) {
+        const int64_t at = kv_at + i / (D / 8) * kv_stride + 8 * (i % (D / 8));
+        *reinterpret_cast<u32x4*>(p.dk + at) = u32x4{0u, 0u, 0u, 0u};
+        *reinterpret_cast<u32x4*>(p.dv + at) = u32x4{0u, 0u, 0u, 0u};
+    }
     if (n == 0) {                                         // no keys: dQ = 0
         for (int i = t_lo * kBM * (D / 8) + tid; i < min(t_hi * kBM, rows_all) * (D / 8); i += kKeysThreads) {
             const int r = i / (D / 8), token = r / G;

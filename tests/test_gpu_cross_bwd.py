@@ -125,6 +125,32 @@ def test_few_items_in_parts_fp32(d):
         assert all(torch.equal(a, b) for a, b in zip(*outs))
 
 
+@pytest.mark.parametrize("n,dtype", [(100, torch.bfloat16), (300, torch.bfloat16), (300, torch.float32)])
+def test_offsets_past_32_bits(n, dtype):
+    """2^31 elements and more in front of the last sequence, of queries (rows of no sequence) and of keys (a padded one)."""
+    far, h, d, lq, scale = 2_200_000, 8, 128, [70, 200], 0.1
+    rnd = lambda *shape: torch.randn(shape, device="cuda").to(dtype)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    q, do, k, v = rnd(270, h, d), rnd(270, h, d), rnd(2 * n, h, d), rnd(2 * n, h, d)
+    cq, ck = i32(0, 70, 270), i32(0, n, 2 * n)
+    o, lse = binding.cross_attn_fwd(q, k, v, cq, ck, 200, n, scale)
+    want = binding.cross_attn_bwd(q, k, v, o, lse, do, cq, ck, 200, n, scale)
+
+    # queries: all behind `far` rows of no sequence; keys: the first sequence's at 0, the last one's behind its padding
+    Q, O, DO = (torch.cat([torch.empty((far, h, d), dtype=dtype, device="cuda"), x]) for x in (q, o, do))
+    LSE = torch.cat([torch.empty((h, far), device="cuda"), lse], dim=1).contiguous()
+    K, V = (torch.cat([x[:n], torch.empty((far - n, h, d), dtype=dtype, device="cuda"), x[n:]]) for x in (k, v))
+    dq, dk, dv = (torch.full_like(x, 7.0) for x in (Q, K, V))
+    binding.cross_attn_bwd(Q, K, V, O, LSE, DO, cq + far, i32(0, far, far + n), 200, n, scale, kv_lens=i32(n, n), dq=dq, dk=dk, dv=dv)
+    assert torch.all(dq[:far] == 7.0)
+    for x in (dk, dv):
+        assert not x[n:far].any()
+    # (the small call may take items in parts: sums in another order, rounded once)
+    step = 2.0 ** -7 if dtype == torch.bfloat16 else 2.0 ** -14
+    for a, b in zip((dq[far:], torch.cat([dk[:n], dk[far:]]), torch.cat([dv[:n], dv[far:]])), want):
+        assert torch.all((a - b).abs() <= step * b.abs() + 2.0 ** -14 * b.abs().max())
+
+
 def test_list_with_many_sequences():
     rng = np.random.default_rng(8)
     for hq, hkv, d in ((8, 8, 64), (6, 3, 128)):
