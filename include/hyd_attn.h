@@ -328,7 +328,7 @@ hyd_status hyd_rope_packed(const void* x, const int32_t* cu_seqlens, int num_seq
  * queries of one request (draft tokens, beams of a search over the same states) let its sequence hold them all.
  *
  *   q, o             device, [total_q][Hq][d];  lse: float [Hq][total_q] (natural log)
- *   k, v             device, [total_kv][Hkv][d]
+ *   k, v             device, [total_kv][Hkv][d]; all four, and the gradients, at multiples of 16 bytes (HYD_ERR_SHAPE)
  *   cu_q, cu_kv      device int32[num_seqs+1], non-decreasing, within 0..total; rows in front of cu[0] and from cu[num_seqs] on
  *                    belong to no sequence: they are not read, and left as they were in the outputs
  *   kv_lens          device int32[num_seqs] or NULL: valid keys of a sequence, for padded caches (cu_kv then holds where each

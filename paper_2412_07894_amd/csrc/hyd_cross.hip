@@ -1,6 +1,7 @@
 // Host side of cross attention (include/hyd_attn.h): argument checks, workspace, choice of the form, launches.
 #include <string.h>
 
+#include <initializer_list>
 #include <mutex>
 
 #include "hyd_cross_bwd.h"
@@ -385,11 +386,13 @@ void launch_bwd_f32(const Sizes& z, const CrossShape& c, const BwdArgs& a, float
 
 // What both directions check before any HIP call; HYD_OK with *nothing set: there is nothing to do.
 hyd_status check_call(const Sizes& z, const int32_t* cu_q, const int32_t* cu_kv, const int32_t* kv_lens, const int32_t* cu_q_host,
-                      const int32_t* cu_kv_host, bool pointers, const void* workspace, size_t bytes, size_t need, bool* nothing) {
+                      const int32_t* cu_kv_host, bool pointers, std::initializer_list<const void*> tensors, const void* workspace, size_t bytes, size_t need, bool* nothing) {
     *nothing = (z.Tq == 0 && z.Tk == 0) || z.nseq == 0;
     if (*nothing) return HYD_OK;
     if (z.Tq > 0 && z.max_q == 0) return HYD_ERR_SHAPE;
     if (!cu_q || !cu_kv || !pointers) return HYD_ERR_NULL;
+    for (const void* t : tensors)
+        if ((uintptr_t)t % 16 != 0) return HYD_ERR_SHAPE;                     // rows are moved 16 bytes at a time
     hyd_status st = check_lengths(cu_q_host, z.nseq, z.Tq, z.max_q, true);
     if (st == HYD_OK) st = check_lengths(cu_kv_host, z.nseq, z.Tk, z.max_kv, kv_lens == nullptr);
     if (st != HYD_OK) return st;
@@ -416,8 +419,8 @@ hyd_status hyd_cross_attn_fwd(const void* q, const void* k, const void* v, const
     if (st != HYD_OK) return st;
     if (total_q == 0) return HYD_OK;
     bool nothing = false;
-    st = check_call(z, cu_q, cu_kv, kv_lens, cu_q_host, cu_kv_host, q && o && lse && (total_kv == 0 || (k && v)), workspace, workspace_bytes,
-                    fwd_layout(z).need, &nothing);
+    st = check_call(z, cu_q, cu_kv, kv_lens, cu_q_host, cu_kv_host, q && o && lse && (total_kv == 0 || (k && v)), {q, k, v, o}, workspace,
+                    workspace_bytes, fwd_layout(z).need, &nothing);
     if (st != HYD_OK || nothing) return st;
     int cus = 0;
     if ((st = cross_device(&cus)) != HYD_OK) return st;
@@ -437,8 +440,8 @@ hyd_status hyd_cross_attn_bwd(const void* q, const void* k, const void* v, const
     if (st != HYD_OK) return st;
     bool nothing = false;
     st = check_call(z, cu_q, cu_kv, kv_lens, cu_q_host, cu_kv_host,
-                    (total_q == 0 || (q && o && lse && d_o && dq)) && (total_kv == 0 || (k && v && dk && dv)), workspace, workspace_bytes,
-                    bwd_layout(z).need, &nothing);
+                    (total_q == 0 || (q && o && lse && d_o && dq)) && (total_kv == 0 || (k && v && dk && dv)),
+                    {q, k, v, o, d_o, dq, dk, dv}, workspace, workspace_bytes, bwd_layout(z).need, &nothing);
     if (st != HYD_OK || nothing) return st;
     int cus = 0;
     if ((st = cross_device(&cus)) != HYD_OK) return st;

@@ -41,6 +41,7 @@ COMMON = [(dict(dt=2), DTYPE), (dict(Tq=-1), SHAPE), (dict(Tk=-1), SHAPE), (dict
           (dict(cq=None), NULL), (dict(ck=None), NULL), (dict(ws=None), WORKSPACE), (dict(ws=P + 64), WORKSPACE), (dict(wb=100), WORKSPACE),
           (dict(Tk=1 << 23, mk=1 << 22), SHAPE),               # 2^22 * 2 * 128 * 2 = 2^31 bytes of keys
           (dict(Tq=1 << 22, mq=1 << 21), SHAPE),               # 2^21 * 4 * 128 * 2 = 2^31 bytes of queries
+          (dict(q=P + 2), SHAPE), (dict(k=P + 8), SHAPE), (dict(v=P + 4), SHAPE),                     # rows move 16 bytes at a time
           (dict(Tq=1 << 30, mq=1), SHAPE),                     # 2^31 packed rows
           (dict(Tq=10, mq=1, hq=1 << 16, hkv=1 << 16), SHAPE)]  # a tile of queries beyond a buffer resource
 SEQ = [([0, 70, 100], None, SHAPE), ([-1, 60, 100], None, SEQLENS), ([0, 60, 101], None, SEQLENS), ([0, 60, 50], None, SEQLENS),

@@ -5,7 +5,7 @@ import torch
 
 from oracle import cross_oracle as co
 from paper_2412_07894_amd import binding
-from cross_util import Case, check_bwd, np64
+from cross_util import Case, check_bwd, cu_of, np64
 
 pytestmark = pytest.mark.gpu
 
@@ -149,6 +149,38 @@ def test_offsets_past_32_bits(n, dtype):
     step = 2.0 ** -7 if dtype == torch.bfloat16 else 2.0 ** -14
     for a, b in zip((dq[far:], torch.cat([dk[:n], dk[far:]]), torch.cat([dv[:n], dv[far:]])), want):
         assert torch.all((a - b).abs() <= step * b.abs() + 2.0 ** -14 * b.abs().max())
+
+
+@pytest.mark.parametrize("hq,hkv", [(64, 1), (192, 2), (128, 1), (300, 1)])
+def test_many_heads_to_a_group(hq, hkv):
+    """Groups of 64 to 300 heads: tokens of a quarter of a tile and of more than a tile, in the general form and with few keys."""
+    for kv in ([50, 0, 128, 77], [50, 0, 300, 77]):
+        both(Case([3, 5, 9, 40], kv, hq, hkv, 64, seed=hq), f"{hq}/{hkv}")
+    both(Case([2, 5, 9], [50, 0, 130], hq, hkv, 64, "fp32", seed=hq), f"{hq}/{hkv}")
+
+
+@pytest.mark.parametrize("longest", [1, 200])
+def test_very_many_sequences(longest):
+    """70000 sequences of one query and one key (one has more): O = V, dV = sum of the group's dO, dQ = dK = 0 there."""
+    n = 70000
+    kv = np.ones(n, dtype=np.int64)
+    kv[n // 2] = longest
+    ck = torch.from_numpy(cu_of(kv)).cuda()
+    cq = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    rnd = lambda t, h: torch.randn((t, h, 64), device="cuda").to(torch.bfloat16)
+    q, k, v, do = rnd(n, 2), rnd(int(kv.sum()), 1), rnd(int(kv.sum()), 1), rnd(n, 2)
+    o, lse = binding.cross_attn_fwd(q, k, v, cq, ck, 1, longest, 0.125)
+    dq, dk, dv = binding.cross_attn_bwd(q, k, v, o, lse, do, cq, ck, 1, longest, 0.125)
+    one = torch.from_numpy(kv == 1).cuda()
+    at = ck[:-1].long()[one]
+    assert torch.equal(o[one], v[at].expand(-1, 2, -1))
+    # scores of one key: LSE is the score, P = 1 within the score's error, 70 * 2^-24 * 0.125 |q| |k| < 1e-4
+    want = do[one].float().sum(1, keepdim=True)
+    size = do[one].float().abs().sum(1, keepdim=True)
+    assert torch.all((dv[at].float() - want).abs() <= 2.0 ** -8 * want.abs() + (2.0 ** -11 + 1e-4) * size)
+    # dP - D: the same 64 products, summed in another order, times P, scale and a k or q of at most 6; in the general form P is an fp16
+    # number and dP - D rounds to nothing above 64 * 2^-24 * sum |do v| < 64 * 2^-24 * 200
+    assert dq[one].float().abs().max() <= 1e-3 and dk[at].float().abs().max() <= 2e-3
 
 
 def test_list_with_many_sequences():
