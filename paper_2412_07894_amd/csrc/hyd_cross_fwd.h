@@ -33,10 +33,12 @@ __device__ __forceinline__ void cross_store_part(float* row, const f32x16 (&acc)
 }
 
 // Work item = (256 packed rows of a sequence and KV head, a part of its keys); 8 waves of 32 rows, K/V tiles of 64 keys through a ring
-// of three stages that all waves share.  Bound by the matrix pipe where rows are many: 6 sequences of 1500 to 6000 queries and 4000 to
-// 12000 keys, 32/8 heads, d = 128, 2.3 ms, 1.15 PFLOP/s (a large bf16 matrix product reaches 1.37).  Short items wait for their first tiles
-// and for their stores: 24 sequences of up to 448 queries and 1500 keys, 20 heads, d = 64, 54 us, and 6 us for their list.  kSelf: one item per workgroup, its sequence and tile from the workgroup's number (launches
+// of three stages that all waves share.  kSelf: one item per workgroup, its sequence and tile from the workgroup's number (launches
 // whose items all fit on the chip, which are too short to wait for a list).
+//
+// Bound by the matrix pipe where rows are many: 6 sequences of 1500 to 6000 queries and 4000 to 12000 keys, 32/8 heads, d = 128, 2.3 ms,
+// 1.15 PFLOP/s (a large bf16 matrix product reaches 1.37).  Short items wait for their first tiles and for their stores: 24
+// sequences of up to 448 queries and 1500 keys, 20 heads, d = 64, 54 us, and 6 us for their list.
 template <int D, bool kSelf>
 __global__ void __launch_bounds__(kFwdThreads, 1) hyd_cross_fwd_bf16_kernel(CrossFwdParams p) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
