@@ -59,12 +59,15 @@ long long most_tiles(long long total, long long most, int nseq, int tile) {
 }
 
 // ---- forward
+// Sequences of at most 128 packed rows in bf16: tiles of as many, two workgroups to a CU (see CrossFwd).
+bool short_rows(const Sizes& z) { return z.dt == HYD_BF16 && (long long)z.max_q * (z.hq / z.hkv) <= CrossFwd<4>::kBM; }
+int fwd_rows(const Sizes& z) { return short_rows(z) ? CrossFwd<4>::kBM : tile_q(z.dt); }
 struct FwdLayout { size_t hdr, items, need, part_o, part_lse, total; long long max_items; };
 constexpr size_t kPartRoomRows = 65536;   // rows (tokens times query heads, times parts) that are joined at most
 FwdLayout fwd_layout(const Sizes& z) {
     FwdLayout w;
     const int G = z.hq / z.hkv;
-    w.max_items = most_tiles((long long)z.Tq * G, (long long)z.max_q * G, z.nseq, tile_q(z.dt));
+    w.max_items = most_tiles((long long)z.Tq * G, (long long)z.max_q * G, z.nseq, fwd_rows(z));
     size_t at = 0;
     w.hdr = at;   at += align_up(sizeof(int) * kHdrTotal);
     w.items = at; at += align_up(16 * (size_t)(w.max_items > 0 ? w.max_items : 1));
@@ -133,7 +136,8 @@ bool allow_lds(K kernel, int lds) {
 }
 template <int D>
 bool prep_kernels() {
-    return allow_lds(hyd_cross_fwd_bf16_kernel<D, false>, kFwdLds) && allow_lds(hyd_cross_fwd_bf16_kernel<D, true>, kFwdLds) &&
+    return allow_lds(hyd_cross_fwd_bf16_kernel<D, false, 8>, CrossFwd<8>::kLds) && allow_lds(hyd_cross_fwd_bf16_kernel<D, true, 8>, CrossFwd<8>::kLds) &&
+           allow_lds(hyd_cross_fwd_bf16_kernel<D, false, 4>, CrossFwd<4>::kLds) && allow_lds(hyd_cross_fwd_bf16_kernel<D, true, 4>, CrossFwd<4>::kLds) &&
            allow_lds(hyd_cross_few_bf16_kernel<D>, kFewLds) && allow_lds(hyd_cross_dq_bf16_kernel<D>, kDqLds) &&
            allow_lds(hyd_cross_bwd_keys_bf16_kernel<D>, KeysForm<D>::kLds) &&
            allow_lds(hyd_bwd_dkdv_wide_bf16_kernel<D, CrossBwdParams>, kKwLds) && allow_lds(hyd_cross_fwd_fp32_kernel<D, false>, f32_lds<D>()) &&
@@ -205,9 +209,11 @@ void launch_fwd(const Sizes& z, const CrossShape& c, const void* q, const void* 
     } else {
         // items of whole tiles: own ones where they all fit on the chip, with the keys in parts where they do not fill it, else from a list
         // (2 x 200 queries of 8/2 heads against 8000 keys, d = 128: 16 parts 34 us, whole 179 us)
-        const int tile = tile_q(z.dt), key_tile = z.dt == HYD_BF16 ? kFwdBN : kF32Tile;
+        const bool small = short_rows(z);
+        const int per_cu = small ? CrossFwd<4>::kPerCu : 1;
+        const int tile = fwd_rows(z), key_tile = z.dt == HYD_BF16 ? kFwdBN : kF32Tile;
         const long long per_seq = tiles(rows, tile), own = (long long)z.nseq * per_seq * z.hkv;
-        const bool self = own <= kCus;
+        const bool self = own <= per_cu * kCus;
         long long want = 1;
         if (self) {
             const long long most = tiles(z.max_kv, 4 * key_tile);
@@ -216,7 +222,7 @@ void launch_fwd(const Sizes& z, const CrossShape& c, const void* q, const void* 
         }
         j.parts = want > 1 ? parts_in_room(w, z, ws_bytes, (int)want) : 1;
         long long grid = self ? own * j.parts : w.max_items * z.hkv;
-        if (!self && grid > cus) grid = cus;
+        if (!self && grid > per_cu * cus) grid = per_cu * cus;
         int* hdr = reinterpret_cast<int*>(ws + w.hdr); int* items = reinterpret_cast<int*>(ws + w.items);
         if (!self) {
             const CrossList l{hdr, items, tile, 1, (int)w.max_items, false};
@@ -233,7 +239,10 @@ void launch_fwd(const Sizes& z, const CrossShape& c, const void* q, const void* 
             common(p);
             p.q = static_cast<const uint16_t*>(q); p.k = static_cast<const uint16_t*>(k); p.v = static_cast<const uint16_t*>(v);
             p.o = static_cast<uint16_t*>(o); p.lse = lse; p.scale_log2 = scale * kLog2eHost;
-            hipLaunchKernelGGL((self ? hyd_cross_fwd_bf16_kernel<D, true> : hyd_cross_fwd_bf16_kernel<D, false>), dim3((unsigned)grid), dim3(kFwdThreads), kFwdLds, st, p);
+            if (small)
+                hipLaunchKernelGGL((self ? hyd_cross_fwd_bf16_kernel<D, true, 4> : hyd_cross_fwd_bf16_kernel<D, false, 4>), dim3((unsigned)grid), dim3(CrossFwd<4>::kThreads), CrossFwd<4>::kLds, st, p);
+            else
+                hipLaunchKernelGGL((self ? hyd_cross_fwd_bf16_kernel<D, true, 8> : hyd_cross_fwd_bf16_kernel<D, false, 8>), dim3((unsigned)grid), dim3(CrossFwd<8>::kThreads), CrossFwd<8>::kLds, st, p);
         } else {
             CrossF32Params p;
             memset(&p, 0, sizeof(p));

@@ -39,11 +39,26 @@ __device__ __forceinline__ void cross_store_part(float* row, const f32x16 (&acc)
 // Bound by the matrix pipe where rows are many: 6 sequences of 1500 to 6000 queries and 4000 to 12000 keys, 32/8 heads, d = 128, 2.3 ms,
 // 1.15 PFLOP/s (a large bf16 matrix product reaches 1.37).  Short items wait for their first tiles and for their stores: 24
 // sequences of up to 448 queries and 1500 keys, 20 heads, d = 64, 54 us, and 6 us for their list.
-template <int D, bool kSelf>
-__global__ void __launch_bounds__(kFwdThreads, 1) hyd_cross_fwd_bf16_kernel(CrossFwdParams p) {
+//
+// NW = 4: 128 rows, two stages, and two workgroups to a CU, one of which streams while the other begins or ends; for sequences that
+// have no more rows.  NW = 8 and 4 with 24 sequences of 1536 keys, 20 heads: 64 queries 52 and 36 us (d = 64), 85 and 79 (128); 128 queries
+// 55 and 38, 91 and 86; 256 queries 73 and 78, 117 and 132.
+template <int NW>
+struct CrossFwd {
+    static constexpr int kBM = 32 * NW, kThreads = 64 * NW, kPerCu = 8 / NW;
+    static constexpr int kStages = NW == 8 ? kFwdStages : 2;
+    static constexpr int kSlotOff = NW == 8 ? kFwdSlotOff : kStages * kFwdStageBytes, kLds = kSlotOff + 128;
+    // where the Q rows of a tile wait, by 64 rows: in what is not a K or V tile's yet
+    __device__ __forceinline__ static constexpr int q_stage(int j) { return NW == 8 ? fwd_q_stage_off(j) : kFwdStageBytes + j * kFwdTileBytes; }
+};
+static_assert(CrossFwd<8>::kLds == kFwdLds && CrossFwd<8>::kBM == kFwdBM && kFwdStages == 3, "the tile form of the self-attention forward");
+
+template <int D, bool kSelf, int NW>
+__global__ void __launch_bounds__(CrossFwd<NW>::kThreads, CrossFwd<NW>::kPerCu) hyd_cross_fwd_bf16_kernel(CrossFwdParams p) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
-    constexpr int kRowB = D * 2;
-    int* slot = reinterpret_cast<int*>(smem + kFwdSlotOff);
+    using F = CrossFwd<NW>;
+    constexpr int kRowB = D * 2, kAhead = F::kStages - 1;             // tiles under way
+    int* slot = reinterpret_cast<int*>(smem + F::kSlotOff);
     volatile int* redo = slot + 16;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -57,7 +72,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) hyd_cross_fwd_bf16_kernel(Cros
     cr.init(G);
     const uint32_t dma_voff = dma_lane_voff<D>(4 * wave + (lane >> 4), lane, kv_stride_b);
     const uint32_t tile_bytes = kFwdBN * kv_stride_b;
-    const int q_stage = fwd_q_stage_off(wave >> 1) + (wave & 1) * 32 * kRowBytes;
+    const int q_stage = F::q_stage(wave >> 1) + (wave & 1) * 32 * kRowBytes;
     const uint32_t o_stage = (uint32_t)(uintptr_t)(lds_char*)smem + (uint32_t)(wave * 32 * kRowBytes);
     const float scale_log2 = fmaxf(fabsf(p.scale_log2), 1e-30f);
     const uint32_t sign_flip = p.scale_log2 < 0.f ? 0x80008000u : 0u;
@@ -71,8 +86,8 @@ __global__ void __launch_bounds__(kFwdThreads, 1) hyd_cross_fwd_bf16_kernel(Cros
         const int part = b % p.parts; b /= p.parts;
         const int tile = b % p.tiles;
         const CrossSeq x = cross_seq(p.c, b / p.tiles);
-        const int left = x.lq * G - tile * kFwdBM;
-        wi.seq = x.q0 * G + tile * kFwdBM; wi.lev = min(left, kFwdBM) | (part << kCrossPartShift); wi.row0 = x.k0; wi.len = x.n;
+        const int left = x.lq * G - tile * F::kBM;
+        wi.seq = x.q0 * G + tile * F::kBM; wi.lev = min(left, F::kBM) | (part << kCrossPartShift); wi.row0 = x.k0; wi.len = x.n;
         have = left > 0;
     } else {
         have = wf.first(p.hm, p.hdr, p.cursors, p.items, slot, wi, blockIdx.x);
@@ -112,19 +127,22 @@ __global__ void __launch_bounds__(kFwdThreads, 1) hyd_cross_fwd_bf16_kernel(Cros
         auto dma_tile = [&](int t, int stage) {
             char* dst = smem + stage * kFwdStageBytes + 4 * wave * kRowBytes;
 #pragma unroll
-            for (int j = 0; j < 16 / kFwdWaves; ++j) {
-                const uint32_t soff = (uint32_t)t * tile_bytes + (uint32_t)(j * kFwdWaves * 4) * kv_stride_b;
-                char* d = dst + j * kFwdWaves * 4 * kRowBytes;
+            for (int j = 0; j < 16 / NW; ++j) {
+                const uint32_t soff = (uint32_t)t * tile_bytes + (uint32_t)(j * NW * 4) * kv_stride_b;
+                char* d = dst + j * NW * 4 * kRowBytes;
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (lds_void*)d, 16, dma_voff, soff, 0, 0);
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void*)(d + kFwdTileBytes), 16, dma_voff, soff, 0, 0);
             }
         };
-        dma_tile(t_lo, 0);
-        if (t_lo + 1 < n_kt) dma_tile(t_lo + 1, 1);
+        const auto dma_first = [&]() {
+            dma_tile(t_lo, 0);
+            if (kAhead > 1 && t_lo + 1 < n_kt) dma_tile(t_lo + 1, 1);
+        };
+        dma_first();
         {
             const uint32_t q_bytes = (uint32_t)((rem + rows - 1) / G) * q_stride_b + (uint32_t)G * kRowB;
-            dma_packed_rows<kFwdWaves, D>(make_rsrc(p.q + (int64_t)t0 * q_stride + (int64_t)g * G * D, q_bytes), smem,
-                                          [](int j) { return fwd_q_stage_off(j); }, (rows + 63) / 64, cr, rem, rows, q_stride_b, wave, lane);
+            dma_packed_rows<NW, D>(make_rsrc(p.q + (int64_t)t0 * q_stride + (int64_t)g * G * D, q_bytes), smem,
+                                          [](int j) { return F::q_stage(j); }, (rows + 63) / 64, cr, rem, rows, q_stride_b, wave, lane);
         }
         if (tid == 0) *redo = 0;
         __syncthreads();                                  // the first tiles and the Q rows have landed
@@ -140,7 +158,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) hyd_cross_fwd_bf16_kernel(Cros
                 qf[ks] = as_bf16x8(qv[ks] ^ sign_flip);
             }
         }
-        __builtin_amdgcn_s_barrier();                     // the staged Q may be overwritten (tile t_lo+2 goes there)
+        __builtin_amdgcn_s_barrier();                     // the staged Q may be overwritten (the next tile goes there)
         const bool short_item = n_kt - t_lo <= kShortItem;
         if (!kSelf && short_item) wf.claim(p.hm, p.cursors);
         // the tile that is masked (see fwd_tile), in a vector register: as a scalar it has the accumulators copied in every tile
@@ -161,20 +179,20 @@ __global__ void __launch_bounds__(kFwdThreads, 1) hyd_cross_fwd_bf16_kernel(Cros
                 for (int r = 0; r < 16; ++r) acc_o[db][r] = 0.f;
             auto step = [&](auto stage_tag, int t) {
                 constexpr int ST = decltype(stage_tag)::value;
-                constexpr int Kt = ST * kFwdStageBytes, Vt = Kt + kFwdTileBytes, ST2 = (ST + 2) % kFwdStages;
-                constexpr int kDmaPerTile = 2 * (16 / kFwdWaves);
-                const bool more2 = t + 2 < n_kt;
-                if (more2) dma_tile(t + 2, ST2);
+                constexpr int Kt = ST * kFwdStageBytes, Vt = Kt + kFwdTileBytes, ST2 = (ST + kAhead) % F::kStages;
+                constexpr int kDmaBehind = (kAhead - 1) * 2 * (16 / NW);      // loads of the tiles behind the next one
+                const bool more = t + kAhead < n_kt;
+                if (more) dma_tile(t + kAhead, ST2);
                 if (active)
                     fwd_tile<D, true>(Kt, Vt, fa, qf, acc_o, m_ref, l_run, scale_log2, t * kFwdBN + koff0, t == td, t, t_find, overflow);
-                if (more2) __builtin_amdgcn_s_waitcnt(0x0070 | (kDmaPerTile & 15));     // vmcnt(kDmaPerTile), lgkmcnt(0)
+                if (more) __builtin_amdgcn_s_waitcnt(0x0070 | (kDmaBehind & 15));       // vmcnt(kDmaBehind), lgkmcnt(0)
                 else __builtin_amdgcn_s_waitcnt(0x0070);                                // vmcnt(0), lgkmcnt(0)
                 __builtin_amdgcn_s_barrier();
             };
-            for (int t = t_lo; t < n_kt; t += 3) {
+            for (int t = t_lo; t < n_kt; t += F::kStages) {
                 step(std::integral_constant<int, 0>{}, t);
                 if (t + 1 < n_kt) step(std::integral_constant<int, 1>{}, t + 1);
-                if (t + 2 < n_kt) step(std::integral_constant<int, 2>{}, t + 2);
+                if (F::kStages > 2 && t + 2 < n_kt) step(std::integral_constant<int, 2 % F::kStages>{}, t + 2);
             }
             if (__any(l_run > kRefQuiet)) overflow |= largest_bits(acc_o) >= kInfBits;
             if (t_find == t_lo && __any(overflow)) *redo = 1;
@@ -183,8 +201,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) hyd_cross_fwd_bf16_kernel(Cros
             t_find = INT_MAX;
             __syncthreads();
             if (tid == 0) *redo = 0;
-            dma_tile(t_lo, 0);
-            if (t_lo + 1 < n_kt) dma_tile(t_lo + 1, 1);
+            dma_first();
             __syncthreads();
         }
         if (!kSelf && !short_item) wf.claim(p.hm, p.cursors);

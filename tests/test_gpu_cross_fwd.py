@@ -53,7 +53,7 @@ def test_scales(lq, scale):
     check_fwd(c, *c.fwd())
 
 
-@pytest.mark.parametrize("lq", [[1, 2, 2], [40, 100, 300]])
+@pytest.mark.parametrize("lq", [[1, 2, 2], [40, 30, 60], [40, 100, 300]])
 @pytest.mark.parametrize("size", [4.0, 16.0, 60.0])
 def test_large_scores(lq, size):
     """Rows whose later keys exceed the first ones by far: the reference of a row has to follow (scores of standard deviation
@@ -62,6 +62,20 @@ def test_large_scores(lq, size):
     for s, a in enumerate(c.ck[:-1]):
         c.k[int(a):int(a) + 64] *= 0.01
     check_fwd(c, *c.fwd())
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_up_to_128_rows(d):
+    """Tiles of 128 rows: own items whole and in parts, a list of them, scores that overflow a first guess, padded keys."""
+    rng = np.random.default_rng(9)
+    for hq, hkv, lq, kv, kw in ((2, 2, [128, 100, 33, 1, 0, 64], [130, 64, 0, 700, 5, 63], {}),
+                                (9, 3, [42, 11, 1], [3000, 200, 1], {}),
+                                (4, 4, [40, 128], [900, 2000], dict(kv_lens=[65, 1900], front=3, back=4)),
+                                (4, 2, [60, 33, 64], [300, 900, 129], dict(size=40.0)),
+                                (2, 2, rng.integers(0, 129, 700), rng.integers(0, 300, 700), {})):
+        c = Case(lq, kv, hq, hkv, d, seed=19, **kw)
+        assert 32 < c.max_q * hq // hkv <= 128
+        check_fwd(c, *c.fwd(), f"{hq}/{hkv}")
 
 
 def test_list_with_many_sequences():
