@@ -34,7 +34,7 @@ inline size_t cross_prep_lds(int hq, int tok) {
 
 template <int D>
 __global__ void __launch_bounds__(kPrepThreads) hyd_cross_prep_bf16_kernel(CrossPrepParams p) {
-    extern __shared__ float st[];                  // [2][hq][tok]: -D, kq
+    extern __shared__ float st[];                  // [2][hq][tok]: -D, the row's largest |dO| as bits
     const int tid = threadIdx.x;
     int wg = blockIdx.x;
     if (wg < kCrossLists) {
@@ -70,7 +70,8 @@ __global__ void __launch_bounds__(kPrepThreads) hyd_cross_prep_bf16_kernel(Cross
         }
         return;
     }
-    // rows of sequences only: what lies outside may be anything, and would enter the maximum
+    // Rows of sequences only: what lies outside may be anything, and would enter the maximum.  Rows without keys (LSE = -inf) have no
+    // part in dK and dV, and none in the maximum either.
     const int T0 = max(p.c.cu_q[0], 0), T1 = min(p.c.cu_q[p.c.nseq], p.c.Tq);
     const int64_t packed = (int64_t)p.c.Tq * G;
     uint32_t gmax = 0;
@@ -107,18 +108,20 @@ __global__ void __launch_bounds__(kPrepThreads) hyd_cross_prep_bf16_kernel(Cross
                 if (c == 0 && r < n_rows) {
                     const int tl = r / hq, h = r - tl * hq;
                     st[h * tok + tl] = -acc;
-                    st[(hq + h) * tok + tl] = (float)shift_of(amax);
+                    st[(hq + h) * tok + tl] = __uint_as_float(amax);
                 }
-                gmax = max(gmax, amax);
             }
         }
         __syncthreads();
         for (int idx = tid; idx < n_rows; idx += kPrepThreads) {      // by packed row
             const int g = idx / (nt * G), i = idx - g * nt * G, tl = i / G, h = g * G + i - tl * G;
             const int64_t at = g * packed + (int64_t)t0 * G + i;
+            const uint32_t amax = __float_as_uint(st[(hq + h) * tok + tl]);
+            const float lse = p.lse[(int64_t)h * p.c.Tq + t0 + tl];
             p.sc.Dq[at] = st[h * tok + tl];
-            p.sc.kqmul[at] = pow2i(-(int)st[(hq + h) * tok + tl]);
-            p.sc.lse2[at] = -p.lse[(int64_t)h * p.c.Tq + t0 + tl] * kLog2e;
+            p.sc.kqmul[at] = pow2i(-shift_of(amax));
+            p.sc.lse2[at] = -lse * kLog2e;
+            if (lse != -INFINITY) gmax = max(gmax, amax);
         }
         __syncthreads();
     }
