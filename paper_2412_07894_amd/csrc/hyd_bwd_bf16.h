@@ -95,8 +95,9 @@ struct PartialMaxima {
 // 262144 tokens, 32/8 heads: 1.11 ms (5.0 TB/s), before 1.10.
 // ---------------------------------------------------------------------------------------------
 constexpr int kPrepThreads = 256, kPrepTarget = 1024;
+constexpr int kPrepRows = 4096;                            // rows whose statistics a workgroup holds: within 32 KB of LDS
 inline int prep_tokens(int T, int hq) {
-    int t = 4096 / (hq > 0 ? hq : 1);                      // statistics of a workgroup within 32 KB of LDS
+    int t = kPrepRows / (hq > 0 ? hq : 1);
     t = t > 32 ? 32 : t;
     const int few = (T + kPrepTarget - 1) / kPrepTarget;
     return t < 1 || few < 1 ? 1 : (t > few ? few : t);

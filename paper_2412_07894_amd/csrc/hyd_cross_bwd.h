@@ -28,13 +28,13 @@ struct CrossPrepParams {
 };
 constexpr int kCrossLists = 2;
 inline size_t cross_prep_lds(int hq, int tok) {
-    const size_t st = sizeof(float) * 2 * (size_t)hq * tok + sizeof(int) * 32;
+    const size_t st = sizeof(float) * 2 * (size_t)(hq < kPrepRows ? hq : kPrepRows) * tok + sizeof(int) * 32;
     return st > (size_t)kCrossListLds ? st : (size_t)kCrossListLds;
 }
 
 template <int D>
 __global__ void __launch_bounds__(kPrepThreads) hyd_cross_prep_bf16_kernel(CrossPrepParams p) {
-    extern __shared__ float st[];                  // [2][hq][tok]: -D, the row's largest |dO| as bits
+    extern __shared__ float st[];                  // [2][heads][tok]: -D, the row's largest |dO| as bits
     const int tid = threadIdx.x;
     int wg = blockIdx.x;
     if (wg < kCrossLists) {
@@ -75,55 +75,59 @@ __global__ void __launch_bounds__(kPrepThreads) hyd_cross_prep_bf16_kernel(Cross
     const int T0 = max(p.c.cu_q[0], 0), T1 = min(p.c.cu_q[p.c.nseq], p.c.Tq);
     const int64_t packed = (int64_t)p.c.Tq * G;
     uint32_t gmax = 0;
+    const int heads = min(hq, kPrepRows);          // of a block; of more heads than that, one token at a time (prep_tokens)
     for (int t0 = T0 + wg * tok; t0 < T1; t0 += p.n_q * tok) {
-        const int nt = min(tok, T1 - t0), n_rows = nt * hq;
-        for (int r0 = grp; r0 < n_rows; r0 += kGrps * kU) {           // row r of the block = (token t0 + r / hq, head r % hq)
-            u32x4 a[kU], b[kU];
+        const int nt = min(tok, T1 - t0);
+        for (int h0 = 0; h0 < hq; h0 += heads) {
+            const int nh = min(heads, hq - h0), n_rows = nt * nh;
+            for (int r0 = grp; r0 < n_rows; r0 += kGrps * kU) {       // row r of the block = (token t0 + r / nh, head h0 + r % nh)
+                u32x4 a[kU], b[kU];
 #pragma unroll
-            for (int u = 0; u < kU; ++u) {
-                const int r = r0 + kGrps * u;
-                a[u] = u32x4{0u, 0u, 0u, 0u};
-                b[u] = u32x4{0u, 0u, 0u, 0u};
-                if (r < n_rows) {
-                    const int64_t at = ((int64_t)t0 * hq + r) * D + c * 8;
-                    a[u] = *reinterpret_cast<const u32x4*>(p.o + at);
-                    b[u] = *reinterpret_cast<const u32x4*>(p.d_o + at);
+                for (int u = 0; u < kU; ++u) {
+                    const int r = r0 + kGrps * u;
+                    a[u] = u32x4{0u, 0u, 0u, 0u};
+                    b[u] = u32x4{0u, 0u, 0u, 0u};
+                    if (r < n_rows) {
+                        const int64_t at = ((int64_t)t0 * hq + h0 + r) * D + c * 8;
+                        a[u] = *reinterpret_cast<const u32x4*>(p.o + at);
+                        b[u] = *reinterpret_cast<const u32x4*>(p.d_o + at);
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < kU; ++u) {
+                    float acc = 0.f;
+                    uint32_t amax = 0;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        acc += bf16_lo(a[u][e]) * bf16_lo(b[u][e]) + bf16_hi(a[u][e]) * bf16_hi(b[u][e]);
+                        amax = max(amax, max(b[u][e] & 0x7fffu, (b[u][e] >> 16) & 0x7fffu));
+                    }
+#pragma unroll
+                    for (int m = 1; m < kLanes; m <<= 1) {
+                        acc += __shfl_xor(acc, m, 64);
+                        amax = max(amax, (uint32_t)__shfl_xor((int)amax, m, 64));
+                    }
+                    const int r = r0 + kGrps * u;
+                    if (c == 0 && r < n_rows) {
+                        const int tl = r / nh, h = r - tl * nh;
+                        st[h * tok + tl] = -acc;
+                        st[(heads + h) * tok + tl] = __uint_as_float(amax);
+                    }
                 }
             }
-#pragma unroll
-            for (int u = 0; u < kU; ++u) {
-                float acc = 0.f;
-                uint32_t amax = 0;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    acc += bf16_lo(a[u][e]) * bf16_lo(b[u][e]) + bf16_hi(a[u][e]) * bf16_hi(b[u][e]);
-                    amax = max(amax, max(b[u][e] & 0x7fffu, (b[u][e] >> 16) & 0x7fffu));
-                }
-#pragma unroll
-                for (int m = 1; m < kLanes; m <<= 1) {
-                    acc += __shfl_xor(acc, m, 64);
-                    amax = max(amax, (uint32_t)__shfl_xor((int)amax, m, 64));
-                }
-                const int r = r0 + kGrps * u;
-                if (c == 0 && r < n_rows) {
-                    const int tl = r / hq, h = r - tl * hq;
-                    st[h * tok + tl] = -acc;
-                    st[(hq + h) * tok + tl] = __uint_as_float(amax);
-                }
+            __syncthreads();
+            for (int idx = tid; idx < n_rows; idx += kPrepThreads) {  // by packed row
+                const int x = h0 + idx, g = x / (nt * G), i = x - g * nt * G, tl = i / G, h = g * G + i - tl * G;
+                const int64_t at = g * packed + (int64_t)t0 * G + i;
+                const uint32_t amax = __float_as_uint(st[(heads + h - h0) * tok + tl]);
+                const float lse = p.lse[(int64_t)h * p.c.Tq + t0 + tl];
+                p.sc.Dq[at] = st[(h - h0) * tok + tl];
+                p.sc.kqmul[at] = pow2i(-shift_of(amax));
+                p.sc.lse2[at] = -lse * kLog2e;
+                if (lse != -INFINITY) gmax = max(gmax, amax);
             }
+            __syncthreads();
         }
-        __syncthreads();
-        for (int idx = tid; idx < n_rows; idx += kPrepThreads) {      // by packed row
-            const int g = idx / (nt * G), i = idx - g * nt * G, tl = i / G, h = g * G + i - tl * G;
-            const int64_t at = g * packed + (int64_t)t0 * G + i;
-            const uint32_t amax = __float_as_uint(st[(hq + h) * tok + tl]);
-            const float lse = p.lse[(int64_t)h * p.c.Tq + t0 + tl];
-            p.sc.Dq[at] = st[h * tok + tl];
-            p.sc.kqmul[at] = pow2i(-shift_of(amax));
-            p.sc.lse2[at] = -lse * kLog2e;
-            if (lse != -INFINITY) gmax = max(gmax, amax);
-        }
-        __syncthreads();
     }
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) gmax = max(gmax, (uint32_t)__shfl_xor((int)gmax, m, 64));
