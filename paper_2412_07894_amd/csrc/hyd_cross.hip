@@ -130,6 +130,9 @@ struct CrossDevice { bool ready = false, ok = false; };
 CrossDevice g_cross[64];
 std::mutex g_cross_mutex;
 
+// A kernel whose input another one of the call should have written is not launched where that launch was refused.
+bool launched() { return hipPeekAtLastError() == hipSuccess; }
+
 template <typename K>
 bool allow_lds(K kernel, int lds) {
     return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess;
@@ -229,6 +232,7 @@ void launch_fwd(const Sizes& z, const CrossShape& c, const void* q, const void* 
             KernelTimer kt("cross_list", st);
             hipLaunchKernelGGL(hyd_cross_list_kernel, dim3(1), dim3(kPreludeThreads), kCrossListLds, st, c, l);
         }
+        if (!launched()) return;
         const auto common = [&](auto& p) {
             p.c = c; p.hdr = hdr; p.cursors = hdr + kHdrCursor; p.items = items; p.hm = head_map_kv(z.hkv, (int)grid);
             p.parts = j.parts; p.tiles = (int)per_seq; p.part_o = const_cast<float*>(j.part_o); p.part_lse = part_lse(j.parts);
@@ -252,7 +256,7 @@ void launch_fwd(const Sizes& z, const CrossShape& c, const void* q, const void* 
             hipLaunchKernelGGL((self ? hyd_cross_fwd_fp32_kernel<D, true> : hyd_cross_fwd_fp32_kernel<D, false>), dim3((unsigned)grid), dim3(64 * kF32Waves), f32_lds<D>(), st, p);
         }
     }
-    if (j.parts > 1) {
+    if (j.parts > 1 && launched()) {
         j.part_lse = part_lse(j.parts);
         if (z.dt == HYD_FP32) launch_join<D, true>(j, st);
         else launch_join<D, false>(j, st);
@@ -292,7 +296,7 @@ void launch_bwd(const Sizes& z, const CrossShape& c, const BwdArgs& a, float sca
             KernelTimer kt("cross_bwd_keys", st);
             hipLaunchKernelGGL(hyd_cross_bwd_keys_bf16_kernel<D>, dim3((unsigned)(items * p.parts)), dim3(kKeysThreads), KeysForm<D>::kLds, st, p);
         }
-        if (p.parts > 1)
+        if (p.parts > 1 && launched())
             launch_sum<D>(CrossSum{part, {p.dk, p.dv}, c.cu_kv, c.kv_lens, z.nseq, z.Tk, z.hkv, p.parts}, false, st);
         return;
     }
@@ -315,6 +319,7 @@ void launch_bwd(const Sizes& z, const CrossShape& c, const BwdArgs& a, float sca
         KernelTimer kt("cross_prep", st);
         hipLaunchKernelGGL(hyd_cross_prep_bf16_kernel<D>, dim3((unsigned)(kCrossLists + p.zero.n + p.n_q + n_k)), dim3(kPrepThreads), cross_prep_lds(z.hq, p.tok), st, p);
     }
+    if (!launched()) return;
     const auto grid_of = [&](long long work) { return (int)(work < 1 ? 1 : (work < cus ? work : cus)); };
     {
         CrossDqParams p;
@@ -327,8 +332,9 @@ void launch_bwd(const Sizes& z, const CrossShape& c, const BwdArgs& a, float sca
         KernelTimer kt("cross_dq", st);
         hipLaunchKernelGGL(hyd_cross_dq_bf16_kernel<D>, dim3(grid), dim3(kDqThreads), kDqLds, st, p, l);
     }
+    if (!launched()) return;
     if (parts_q > 1) launch_sum<D>(CrossSum{part, {a.dq, nullptr}, c.cu_q, nullptr, z.nseq, z.Tq, z.hq, parts_q}, false, st);
-    if (z.Tk == 0) return;
+    if (z.Tk == 0 || !launched()) return;
     {
         CrossBwdParams p;
         memset(&p, 0, sizeof(p));
@@ -343,7 +349,7 @@ void launch_bwd(const Sizes& z, const CrossShape& c, const BwdArgs& a, float sca
         KernelTimer kt("cross_dkdv", st);
         hipLaunchKernelGGL((hyd_bwd_dkdv_wide_bf16_kernel<D, CrossBwdParams>), dim3(grid), dim3(kKwThreads), kKwLds, st, p, l);
     }
-    if (parts_kv > 1)
+    if (parts_kv > 1 && launched())
         launch_sum<D>(CrossSum{part, {a.dk, a.dv}, c.cu_kv, c.kv_lens, z.nseq, z.Tk, z.hkv, parts_kv}, false, st);
 }
 
@@ -365,6 +371,7 @@ void launch_bwd_f32(const Sizes& z, const CrossShape& c, const BwdArgs& a, float
         KernelTimer kt("cross_begin", st);
         hipLaunchKernelGGL(hyd_cross_begin_fp32_kernel, dim3(2 + b.zero.n), dim3(kPreludeThreads), kCrossListLds, st, b);
     }
+    if (!launched()) return;
     CrossF32Params p;
     memset(&p, 0, sizeof(p));
     p.c = c; p.scale = scale; p.part_o = part;
@@ -383,6 +390,7 @@ void launch_bwd_f32(const Sizes& z, const CrossShape& c, const BwdArgs& a, float
         KernelTimer kt("cross_dq", st);
         hipLaunchKernelGGL(hyd_cross_dq_fp32_kernel<D>, dim3(grid), dim3(64 * kF32Waves), f32_lds<D>(), st, p);
     }
+    if (!launched()) return;
     if (parts_q > 1) launch_sum<D>(CrossSum{part, {a.dq, nullptr}, c.cu_q, nullptr, z.nseq, z.Tq, z.hq, parts_q}, true, st);
     const int grid = take(1, w.n_kv * z.hkv * parts_kv);
     p.parts = parts_kv;
@@ -390,7 +398,7 @@ void launch_bwd_f32(const Sizes& z, const CrossShape& c, const BwdArgs& a, float
         KernelTimer kt("cross_dkdv", st);
         hipLaunchKernelGGL((parts_kv > 1 ? hyd_cross_dkdv_fp32_kernel<D, true> : hyd_cross_dkdv_fp32_kernel<D, false>), dim3(grid), dim3(64 * kF32KvWaves), f32_lds<D>(), st, p);
     }
-    if (parts_kv > 1) launch_sum<D>(CrossSum{part, {a.dk, a.dv}, c.cu_kv, c.kv_lens, z.nseq, z.Tk, z.hkv, parts_kv}, true, st);
+    if (parts_kv > 1 && launched()) launch_sum<D>(CrossSum{part, {a.dk, a.dv}, c.cu_kv, c.kv_lens, z.nseq, z.Tk, z.hkv, parts_kv}, true, st);
 }
 
 // What both directions check before any HIP call; HYD_OK with *nothing set: there is nothing to do.
