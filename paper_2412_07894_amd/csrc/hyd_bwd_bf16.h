@@ -107,7 +107,7 @@ inline int prep_workgroups(int T, int tok) {
     return n < kPrepMaxWg ? n : kPrepMaxWg;
 }
 inline size_t prep_lds(int hq, int tok, size_t schedule) {
-    const size_t st = sizeof(float) * 2 * (size_t)hq * tok + sizeof(int) * 32;
+    const size_t st = sizeof(float) * 2 * (size_t)(hq < kPrepRows ? hq : kPrepRows) * tok + sizeof(int) * 32;
     return st > schedule ? st : schedule;
 }
 struct PrepParams {
@@ -124,7 +124,7 @@ struct PrepParams {
 // kCopyQ: the fp16 copy of Q too, for a dK/dV that runs beside dQ (small batches)
 template <bool R, int HD = kHeadDim, bool kCopyQ = false>
 __global__ void __launch_bounds__(kPrepThreads) hyd_bwd_prep_bf16_kernel(PrepParams p) {
-    extern __shared__ float st[];                  // [2][hq][tok]: -D, kq; then [tok] row flags (range variant)
+    extern __shared__ float st[];                  // [2][heads][tok]: -D, kq; then [tok] row flags (range variant)
     const int tid = threadIdx.x;
     if ((int)blockIdx.x < p.n_sched) {
         const int w = blockIdx.x;
@@ -136,7 +136,8 @@ __global__ void __launch_bounds__(kPrepThreads) hyd_bwd_prep_bf16_kernel(PrepPar
     }
     const int wg = blockIdx.x - p.n_sched, n_wg = gridDim.x - p.n_sched;
     const int T = p.T, hq = p.hq, hkv = p.hkv, tok = p.tok;
-    int* flags = reinterpret_cast<int*>(st + 2 * hq * tok);
+    const int heads = min(hq, kPrepRows);          // of a block; of more heads than that, one token at a time (prep_tokens)
+    int* flags = reinterpret_cast<int*>(st + 2 * heads * tok);
     constexpr int kLanes = HD / 8, kGrps = kPrepThreads / kLanes;       // lanes per row, rows at a time
     const int grp = tid / kLanes, c = tid % kLanes;
     uint32_t gmax = 0;
@@ -158,82 +159,84 @@ __global__ void __launch_bounds__(kPrepThreads) hyd_bwd_prep_bf16_kernel(PrepPar
             __syncthreads();
         }
         constexpr int kU = 4;                      // rows in flight
-        const int n_rows = nt * hq;
-        for (int r0 = grp; r0 < n_rows; r0 += kGrps * kU) {       // row r of the block = (token t0 + r / hq, head r % hq)
-            u32x4 a[kU], b[kU], q[kU];
-            bool on[kU];
+        for (int h0 = 0; h0 < hq; h0 += heads) {
+            const int nh = min(heads, hq - h0), n_rows = nt * nh;
+            for (int r0 = grp; r0 < n_rows; r0 += kGrps * kU) {       // row r of the block = (token t0 + r / nh, head h0 + r % nh)
+                u32x4 a[kU], b[kU], q[kU];
+                bool on[kU];
 #pragma unroll
-            for (int u = 0; u < kU; ++u) {
-                const int r = r0 + kGrps * u;
-                on[u] = r < n_rows && (!R || (flags[r / hq] & 1));
-                a[u] = u32x4{0u, 0u, 0u, 0u};
-                b[u] = u32x4{0u, 0u, 0u, 0u};
-                if (kCopyQ && on[u]) q[u] = *reinterpret_cast<const u32x4*>(p.q + ((int64_t)t0 * hq + r) * HD + c * 8);
-                if (on[u]) {
-                    const int64_t at = ((int64_t)t0 * hq + r) * HD + c * 8;
-                    a[u] = *reinterpret_cast<const u32x4*>(p.o + at);
-                    b[u] = *reinterpret_cast<const u32x4*>(p.d_o + at);
+                for (int u = 0; u < kU; ++u) {
+                    const int r = r0 + kGrps * u;
+                    on[u] = r < n_rows && (!R || (flags[r / nh] & 1));
+                    a[u] = u32x4{0u, 0u, 0u, 0u};
+                    b[u] = u32x4{0u, 0u, 0u, 0u};
+                    if (kCopyQ && on[u]) q[u] = *reinterpret_cast<const u32x4*>(p.q + ((int64_t)t0 * hq + h0 + r) * HD + c * 8);
+                    if (on[u]) {
+                        const int64_t at = ((int64_t)t0 * hq + h0 + r) * HD + c * 8;
+                        a[u] = *reinterpret_cast<const u32x4*>(p.o + at);
+                        b[u] = *reinterpret_cast<const u32x4*>(p.d_o + at);
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < kU; ++u) {
+                    float acc = 0.f;
+                    uint32_t amax = 0;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        acc += bf16_lo(a[u][e]) * bf16_lo(b[u][e]) + bf16_hi(a[u][e]) * bf16_hi(b[u][e]);
+                        amax = max(amax, max(b[u][e] & 0x7fffu, (b[u][e] >> 16) & 0x7fffu));
+                    }
+#pragma unroll
+                    for (int m = 1; m < kLanes; m <<= 1) {
+                        acc += __shfl_xor(acc, m, 64);
+                        amax = max(amax, (uint32_t)__shfl_xor((int)amax, m, 64));
+                    }
+                    const int r = r0 + kGrps * u;
+                    if (c == 0 && on[u]) {
+                        const int tl = r / nh, h = r - tl * nh;
+                        st[h * tok + tl] = -acc;
+                        st[(heads + h) * tok + tl] = (float)shift_of(amax);
+                    }
+                    gmax = max(gmax, amax);
+                    if (kCopyQ && on[u]) {
+                        u32x4 q16;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) q16[e] = bf16x2_to_f16x2(q[u][e]);
+                        *reinterpret_cast<u32x4*>(p.sc.q16 + ((int64_t)t0 * hq + h0 + r) * HD + c * 8) = q16;
+                    }
                 }
             }
+            for (int r0 = grp; h0 == 0 && r0 < nt * hkv; r0 += kGrps * kU) {     // the K rows of the same tokens
+                u32x4 x[kU];
+                bool on[kU];
 #pragma unroll
-            for (int u = 0; u < kU; ++u) {
-                float acc = 0.f;
-                uint32_t amax = 0;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    acc += bf16_lo(a[u][e]) * bf16_lo(b[u][e]) + bf16_hi(a[u][e]) * bf16_hi(b[u][e]);
-                    amax = max(amax, max(b[u][e] & 0x7fffu, (b[u][e] >> 16) & 0x7fffu));
+                for (int u = 0; u < kU; ++u) {
+                    const int r = r0 + kGrps * u;
+                    on[u] = r < nt * hkv && (!R || (flags[r / hkv] & 2));
+                    if (on[u]) x[u] = *reinterpret_cast<const u32x4*>(p.k + ((int64_t)t0 * hkv + r) * HD + c * 8);
                 }
 #pragma unroll
-                for (int m = 1; m < kLanes; m <<= 1) {
-                    acc += __shfl_xor(acc, m, 64);
-                    amax = max(amax, (uint32_t)__shfl_xor((int)amax, m, 64));
-                }
-                const int r = r0 + kGrps * u;
-                if (c == 0 && on[u]) {
-                    const int tl = r / hq, h = r - tl * hq;
-                    st[h * tok + tl] = -acc;
-                    st[(hq + h) * tok + tl] = (float)shift_of(amax);
-                }
-                gmax = max(gmax, amax);
-                if (kCopyQ && on[u]) {
-                    u32x4 q16;
+                for (int u = 0; u < kU; ++u) {
+                    if (on[u]) {
+                        u32x4 x16;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) q16[e] = bf16x2_to_f16x2(q[u][e]);
-                    *reinterpret_cast<u32x4*>(p.sc.q16 + ((int64_t)t0 * hq + r) * HD + c * 8) = q16;
+                        for (int e = 0; e < 4; ++e) x16[e] = bf16x2_to_f16x2(x[u][e]);
+                        *reinterpret_cast<u32x4*>(p.sc.k16 + ((int64_t)t0 * hkv + r0 + kGrps * u) * HD + c * 8) = x16;
+                    }
                 }
             }
+            __syncthreads();
+            for (int idx = tid; idx < nh * tok; idx += kPrepThreads) {
+                const int h = idx / tok, tl = idx % tok;
+                if (tl < nt && (!R || (flags[tl] & 1))) {
+                    const int64_t at = (int64_t)(h0 + h) * T + t0 + tl;
+                    p.sc.Dq[at] = st[idx];
+                    p.sc.kqmul[at] = pow2i(-(int)st[heads * tok + idx]);
+                    p.sc.lse2[at] = -p.lse[at] * kLog2e;
+                }
+            }
+            __syncthreads();                           // st and flags are free again
         }
-        for (int r0 = grp; r0 < nt * hkv; r0 += kGrps * kU) {     // the K rows of the same tokens
-            u32x4 x[kU];
-            bool on[kU];
-#pragma unroll
-            for (int u = 0; u < kU; ++u) {
-                const int r = r0 + kGrps * u;
-                on[u] = r < nt * hkv && (!R || (flags[r / hkv] & 2));
-                if (on[u]) x[u] = *reinterpret_cast<const u32x4*>(p.k + ((int64_t)t0 * hkv + r) * HD + c * 8);
-            }
-#pragma unroll
-            for (int u = 0; u < kU; ++u) {
-                if (on[u]) {
-                    u32x4 x16;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) x16[e] = bf16x2_to_f16x2(x[u][e]);
-                    *reinterpret_cast<u32x4*>(p.sc.k16 + ((int64_t)t0 * hkv + r0 + kGrps * u) * HD + c * 8) = x16;
-                }
-            }
-        }
-        __syncthreads();
-        for (int idx = tid; idx < hq * tok; idx += kPrepThreads) {
-            const int h = idx / tok, tl = idx % tok;
-            if (tl < nt && (!R || (flags[tl] & 1))) {
-                const int64_t at = (int64_t)h * T + t0 + tl;
-                p.sc.Dq[at] = st[idx];
-                p.sc.kqmul[at] = pow2i(-(int)st[hq * tok + idx]);
-                p.sc.lse2[at] = -p.lse[at] * kLog2e;
-            }
-        }
-        __syncthreads();                           // st and flags are free again
     }
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) gmax = max(gmax, (uint32_t)__shfl_xor((int)gmax, m, 64));
