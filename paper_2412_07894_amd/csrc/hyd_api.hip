@@ -427,6 +427,10 @@ hyd_status device_info(DeviceInfo** out) {
     return HYD_OK;
 }
 
+// A kernel whose input another one of the call should have written is not launched where that launch was refused.
+bool launched() { return hipPeekAtLastError() == hipSuccess; }
+hyd_status launch_error() { (void)hipGetLastError(); return HYD_ERR_LAUNCH; }
+
 // ---- benchmark hooks --------------------------------------------------------------------------
 thread_local bool t_timing = false;
 thread_local std::vector<TimedKernel> t_timed;
@@ -683,6 +687,7 @@ hyd_status fwd_impl(const void* q, const void* k, const void* v, const int32_t* 
                            total_tokens, tile, sv_whole, tile >> shift, sv,
                            rope_tab, head_dim / 2, rope_base != 0.f ? log2((double)rope_base) : 0.0);
     }
+    if (!launched()) return launch_error();
     if (dt == HYD_BF16) {
         FwdParams p;
         p.q = static_cast<const uint16_t*>(q); p.k = static_cast<const uint16_t*>(k);
@@ -802,6 +807,7 @@ hyd_status bwd_impl(const void* q, const void* k, const void* v, const void* o, 
                          : (head_dim == 64 ? hyd_bwd_prep_bf16_kernel<false, 64> : hyd_bwd_prep_bf16_kernel<false, 128>);
             hipLaunchKernelGGL(kernel, grid, block, lds, st, pp);
         }
+        if (!launched()) return launch_error();
         BwdParams p;
         p.q = static_cast<const uint16_t*>(q); p.v = static_cast<const uint16_t*>(v); p.d_o = static_cast<const uint16_t*>(d_o);
         p.sc = sc;
@@ -830,6 +836,7 @@ hyd_status bwd_impl(const void* q, const void* k, const void* v, const void* o, 
                 KernelTimer kt(ranged ? "bwd_dq_range_bf16" : "bwd_dq_bf16", st);
                 hipLaunchKernelGGL(kDqKernels[ranged ? 3 : split][head_dim == 64], dim3(grid_q), dim3(kDqThreads), kDqLds, st, p, lq);
             }
+            if (!launched()) return launch_error();
             KernelTimer kt(ranged ? "bwd_dkdv_range_bf16" : "bwd_dkdv_bf16", st);
             const BwdKernel kernel = ranged ? (head_dim == 64 ? hyd_bwd_dkdv_bf16_kernel<true, 64> : hyd_bwd_dkdv_bf16_kernel<true, 128>)
                                             : (head_dim == 64 ? hyd_bwd_dkdv_bf16_kernel<false, 64> : hyd_bwd_dkdv_bf16_kernel<false, 128>);
@@ -840,7 +847,7 @@ hyd_status bwd_impl(const void* q, const void* k, const void* v, const void* o, 
             }
             if (wide != kKvWide) hipLaunchKernelGGL(kernel, dim3(grid_kv), dim3(kKvThreads), kKvLds, st, p, lkv);
         }
-        if (sv_kv.part_max > 1) {
+        if (sv_kv.part_max > 1 && launched()) {
             SumParams sp;
             sp.part = p.part; sp.dk = p.dk; sp.dv = p.dv; sp.T = total_tokens; sp.hkv = hkv;
             sp.part_max = sv_kv.part_max; sp.part_q = sv_kv.part_q; sp.steps_per_level = sv_kv.steps_per_level;
@@ -870,6 +877,7 @@ hyd_status bwd_impl(const void* q, const void* k, const void* v, const void* o, 
             hipLaunchKernelGGL(hyd_schedule_prelude, dim3(w.n_sched), dim3(kPreludeThreads), schedule_lds(sv_kv.n_lev, sv_q.n_lev), st, cu_seqlens,
                                num_seqs, total_tokens, tile_kv(dt), sv_kv, tile_q(dt), sv_q, nullptr, 0, 0.0);
         }
+        if (!launched()) return launch_error();
         const dim3 grid_q(persistent_grid(*dev, occ_q, work_q)), grid_kv(persistent_grid(*dev, occ_kv, work_kv));
         // dQ first: it also writes the row sums D that dK/dV reads
         {
@@ -885,7 +893,7 @@ hyd_status bwd_impl(const void* q, const void* k, const void* v, const void* o, 
             else if (short_rows) hipLaunchKernelGGL((hyd_bwd_dq_fp32_kernel<128, true>), grid_q, dim3(64 * kF32Waves), f32_rows_lds(), st, p);
             else hipLaunchKernelGGL(hyd_bwd_dq_fp32_kernel<128>, grid_q, dim3(64 * kF32Waves), f32_lds<128>(), st, p);
         }
-        {
+        if (launched()) {
             p.hdr = sv_kv.hdr; p.items = sv_kv.exec; p.cursors = sv_kv.hdr + kHdrCursor; p.hm = head_map_kv(hkv, grid_kv.x);
             KernelTimer kt("bwd_dkdv_fp32", st);
             if (head_dim == 64) hipLaunchKernelGGL(hyd_bwd_dkdv_fp32_kernel<64>, grid_kv, dim3(64 * kF32KvWaves), f32_lds<64>(), st, p);
