@@ -169,6 +169,10 @@ CrossShape shape_of(const Sizes& z, const int32_t* cu_q, const int32_t* cu_kv, c
     return c;
 }
 
+// A launch has fewer than 2^32 threads.  The forms that give a workgroup to every (sequence, KV head) leave more of them to those
+// that take items from a list.
+bool fits_launch(long long workgroups, int threads) { return workgroups * threads < (1ll << 32); }
+
 template <int D, bool kF32>
 void launch_join(const CrossJoin& j, hipStream_t st) {
     KernelTimer kt("cross_join", st);
@@ -184,14 +188,13 @@ void launch_fwd(const Sizes& z, const CrossShape& c, const void* q, const void* 
     CrossJoin j;
     j.part_o = reinterpret_cast<float*>(ws + w.need);
     j.o = o; j.lse = lse; j.cu_q = c.cu_q; j.nseq = z.nseq; j.Tq = z.Tq; j.hq = z.hq; j.parts = 1;
-    const long long rows = (long long)z.max_q * c.G;
+    const long long rows = (long long)z.max_q * c.G, items = (long long)z.nseq * z.hkv;
     const auto part_lse = [&](int parts) { return reinterpret_cast<float*>(ws + w.need + align_up((size_t)parts * z.Tq * z.hq * z.d * 4)); };
-    if (z.dt == HYD_BF16 && rows <= kFewRows) {
+    if (z.dt == HYD_BF16 && rows <= kFewRows && fits_launch(items, kFewThreads)) {
         CrossFewParams p;
         p.c = c;
         p.q = static_cast<const uint16_t*>(q); p.k = static_cast<const uint16_t*>(k); p.v = static_cast<const uint16_t*>(v);
         p.o = static_cast<uint16_t*>(o); p.lse = lse; p.scale_log2 = scale * kLog2eHost;
-        const long long items = (long long)z.nseq * z.hkv;
         constexpr int kTurn = kFewWaves * kFewKeys;
         // Parts of the keys: two workgroups for a CU, or if there are as many items as CUs, 32, whose ends then hardly differ;
         // each of 512 keys at least (1024 where the chip is full).  Up to 1024 keys (2048) they stay whole: a second launch costs 3 us.
@@ -283,18 +286,18 @@ void launch_bwd(const Sizes& z, const CrossShape& c, const BwdArgs& a, float sca
     const size_t room = ws_bytes - w.need, q_rows = (size_t)z.Tq * z.hq, kv_rows = (size_t)z.Tk * z.hkv;
     const int parts_q = bwd_parts(w.n_q * z.hkv, kCus, tiles(z.max_kv, kDqBN), 8, q_rows, kDqPartRows, (size_t)D * 4, room);
     const int parts_kv = bwd_parts(w.n_kv * z.hkv, kBwdItems, tiles((long long)z.max_q * G, kKwBM), 8, kv_rows, kKvPartRows, (size_t)D * 8, room);
-    if (z.max_kv <= kKeysMax && z.max_kv > 0) {
+    const long long pairs = (long long)z.nseq * z.hkv;
+    if (z.max_kv <= kKeysMax && z.max_kv > 0 && fits_launch(pairs, kKeysThreads)) {
         CrossKeysParams p;
         p.c = c;
         p.q = static_cast<const uint16_t*>(a.q); p.k = static_cast<const uint16_t*>(a.k); p.v = static_cast<const uint16_t*>(a.v);
         p.o = static_cast<const uint16_t*>(a.o); p.d_o = static_cast<const uint16_t*>(a.d_o); p.lse = a.lse;
         p.dq = static_cast<uint16_t*>(a.dq); p.dk = static_cast<uint16_t*>(a.dk); p.dv = static_cast<uint16_t*>(a.dv);
-        const long long items = (long long)z.nseq * z.hkv;
-        p.parts = bwd_parts(items, kBwdItems, tiles((long long)z.max_q * G, KeysForm<D>::kBM), 4, kv_rows, kKvPartRows, (size_t)D * 8, room);
+        p.parts = bwd_parts(pairs, kBwdItems, tiles((long long)z.max_q * G, KeysForm<D>::kBM), 4, kv_rows, kKvPartRows, (size_t)D * 8, room);
         p.part = part; p.scale = scale; p.scale_log2 = scale * kLog2eHost;
         {
             KernelTimer kt("cross_bwd_keys", st);
-            hipLaunchKernelGGL(hyd_cross_bwd_keys_bf16_kernel<D>, dim3((unsigned)(items * p.parts)), dim3(kKeysThreads), KeysForm<D>::kLds, st, p);
+            hipLaunchKernelGGL(hyd_cross_bwd_keys_bf16_kernel<D>, dim3((unsigned)(pairs * p.parts)), dim3(kKeysThreads), KeysForm<D>::kLds, st, p);
         }
         if (p.parts > 1 && launched())
             launch_sum<D>(CrossSum{part, {p.dk, p.dv}, c.cu_kv, c.kv_lens, z.nseq, z.Tk, z.hkv, p.parts}, false, st);
