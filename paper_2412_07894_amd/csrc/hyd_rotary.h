@@ -19,6 +19,7 @@ namespace hyd {
 
 constexpr int kRotThreads = 256, kRotTokens = 16, kRotAhead = 4;
 constexpr int kRotMaxDim = 1024;          // elements of a head
+constexpr int kRotGridX = 1 << 22;        // workgroups of a grid's row (a launch has fewer than 2^32 threads in one dimension)
 
 struct RotTensor { const void* x; void* out; int64_t x_stride, out_stride; int heads; };      // strides of a token in elements
 struct RotParams {
@@ -52,7 +53,9 @@ __global__ void __launch_bounds__(kRotThreads) hyd_rotary_kernel(RotParams p) {
     __shared__ long long pos[kRotTokens];                // of the workgroup's rows; kNone: in no sequence
     constexpr long long kNone = INT64_MIN;
     const int tid = threadIdx.x, half = p.rot / 2;
-    const int t0 = blockIdx.x * p.tok, nt = min(p.tok, p.T - t0);
+    const int64_t begin = ((int64_t)blockIdx.y * kRotGridX + blockIdx.x) * p.tok;
+    if (begin >= p.T) return;
+    const int t0 = (int)begin, nt = min(p.tok, p.T - t0);
     const int H = p.t[0].heads + p.t[1].heads;
     const int n_units = nt * H * p.units;
     const float inv_units = 1.f / (float)p.units, inv_h = 1.f / (float)H;

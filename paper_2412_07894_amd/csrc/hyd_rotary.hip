@@ -89,7 +89,8 @@ hyd_status hyd_rope_rotate(const void* q, int hq, int64_t q_stride, void* q_out,
     // 18.2 and 22.9 us, 24700 tokens 109, 106 and 123 us.
     p.tok = 1;
     while (2 * p.tok <= kRotTokens && 2ll * p.tok * cus * 16 <= total_tokens && 2 * p.tok * row_units <= (1 << 20)) p.tok *= 2;
-    const dim3 grid((unsigned)((total_tokens + p.tok - 1) / p.tok));
+    const unsigned groups = (unsigned)((total_tokens + (long long)p.tok - 1) / p.tok);
+    const dim3 grid(groups < kRotGridX ? groups : kRotGridX, (groups + kRotGridX - 1) / kRotGridX);
     const size_t lds = sizeof(float) * 2 * (size_t)p.tok * (size_t)(rot_dim / 2);
     const bool side = layout == HYD_ROPE_INTERLEAVED;
     const RotKernel kernel = dt == HYD_BF16 ? (c == 8 ? rot_kernel<uint16_t, 8>(side) : c == 4 ? rot_kernel<uint16_t, 4>(side)

@@ -1,6 +1,4 @@
 """General rotary positions where a workgroup takes its most rows: from 65536 rows on sixteen of them, small heads and the widest."""
-import math
-
 import pytest
 import torch
 
@@ -48,3 +46,30 @@ def test_many_rows(heads, d, rot, layout, dtype):
     pos = t - cu[:-1].long()[(t[:, None] >= cu[1:].long()[None]).sum(1)]
     for a in range(0, T, 8192):
         check(y[a:a + 8192], x[a:a + 8192], pos[a:a + 8192], freqs, layout, dtype)
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_more_rows_than_a_launch_has_threads_for(layout):
+    """2^28 rows and more, sixteen to a workgroup of 256 threads: 2^32 threads."""
+    T, first = 2 ** 28 + 37, 100_000_000
+    g = torch.Generator(device="cuda")
+    g.manual_seed(6)
+    x = torch.randn((T, 1, 2), generator=g, device="cuda", dtype=torch.bfloat16)
+    cu = torch.tensor([0, first, T], dtype=torch.int32, device="cuda")
+    freqs = binding.rope_frequencies(2)
+    y = binding.rope_rotate(x, freqs, cu_seqlens=cu, layout=layout)
+    step = 1 << 24
+    for a in range(0, T, step):
+        t = torch.arange(a, min(a + step, T), device="cuda")
+        check(y[a:a + step], x[a:a + step], torch.where(t < first, t, t - first), freqs, layout, "bf16")
+
+
+def test_second_row_of_workgroups():
+    """2^22 workgroups of sixteen rows, and one row more: the grid gets its second row."""
+    freqs = binding.rope_frequencies(2)
+    for T in (2 ** 26, 2 ** 26 + 1):
+        x = torch.randn((T, 1, 2), device="cuda", dtype=torch.bfloat16)
+        pos = torch.arange(T, dtype=torch.int32, device="cuda")
+        y = binding.rope_rotate(x, freqs, positions=pos)
+        for a in range(0, T, 1 << 24):
+            check(y[a:a + (1 << 24)], x[a:a + (1 << 24)], pos[a:a + (1 << 24)], freqs, "half", "bf16")
