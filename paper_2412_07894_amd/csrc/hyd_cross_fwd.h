@@ -397,7 +397,7 @@ __global__ void __launch_bounds__(kFewThreads, 2) hyd_cross_few_bf16_kernel(Cros
     float top = -INFINITY;
 #pragma unroll
     for (int w = 0; w < kFewWaves; ++w) top = fmaxf(top, ml[w * 2 * kFewRows + l32]);
-    const float w_mine = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+    const float w_mine = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(m - top);      // (l = 0: no keys; m = -inf alone may be a row of nan)
     const uint32_t sums = (uint32_t)(uintptr_t)(lds_char*)smem;
     if (l32 < rows) {
 #pragma unroll
@@ -417,8 +417,8 @@ __global__ void __launch_bounds__(kFewThreads, 2) hyd_cross_few_bf16_kernel(Cros
         f32x4 sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < kFewWaves; ++w) {
-            const float mw = ml[w * 2 * kFewRows + r];
-            lt += mw == -INFINITY ? 0.f : ml[w * 2 * kFewRows + kFewRows + r] * __builtin_amdgcn_exp2f(mw - mt);
+            const float lw = ml[w * 2 * kFewRows + kFewRows + r];
+            lt += lw == 0.f ? 0.f : lw * __builtin_amdgcn_exp2f(ml[w * 2 * kFewRows + r] - mt);
             sum += *(lds_f32x4*)(uintptr_t)(sums + (uint32_t)(w * kFewWaveBytes + r * D * 4 + ((c ^ (r & 15)) << 4)));
         }
         const float inv = lt == 0.f ? 0.f : 1.f / lt, log2_sum = lt == 0.f ? -INFINITY : mt + __builtin_amdgcn_logf(lt);

@@ -53,3 +53,33 @@ def test_more_heads_than_one_pass_over_statistics_holds(hq, hkv, d):
     for name, got, want in zip(("dq", "dk", "dv"), c.bwd(o, lse), dense(c, o, lse)):
         # one rounding of 2^-8 / sqrt(3) * 0.74, those to fp16 are an eighth of it; a quarter more (see cross_util)
         assert float((got.double() - want).norm() / want.norm()) < 1.25 * 0.74 * 2.0 ** -8 / 3 ** 0.5, name
+
+
+def marked(c, kind):
+    """nan in one query row (kind "q"), in all valid keys of a sequence ("all"), or in one run of 32 keys, a wave's turn in the form
+    for few rows ("run"); O and LSE of the rows that see it are nan, all others as they were."""
+    if kind == "q":
+        c.q[int(c.cq[1]), 1] = float("nan")
+        rows, heads = slice(int(c.cq[1]), int(c.cq[1]) + 1), slice(1, 2)
+    else:
+        a = int(c.ck[1])
+        c.k[a:a + c.n[1], 0] = c.k[a:a + c.n[1], 0] if kind == "run" else float("nan")
+        if kind == "run":
+            c.k[a + 32:a + 64, 0] = float("nan")
+        rows, heads = slice(int(c.cq[1]), int(c.cq[2])), slice(0, c.hq // c.hkv)
+    hit = torch.zeros((c.Tq, c.hq), dtype=torch.bool, device="cuda")
+    hit[rows, heads] = True
+    return hit
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("kind", ["q", "all", "run"])
+@pytest.mark.parametrize("lq,kv", [([1, 2, 1], [70, 90, 5]), ([1, 2, 1], [3000, 2100, 5]), ([40, 30, 7], [70, 90, 5]), ([200, 300, 1], [3000, 2100, 5]),
+                                   ([40, 3, 64], [2000, 3000, 77])])
+def test_nan_stays_nan_and_where_it_is(lq, kv, kind, dtype):
+    c = Case(lq, kv, 4, 2, 64, dtype, seed=33)
+    o, lse = c.fwd()
+    hit = marked(c, kind)
+    o2, lse2 = c.fwd()
+    assert torch.all(torch.isnan(o2[hit])) and torch.all(torch.isnan(lse2.t()[hit]))
+    assert torch.equal(o2[~hit], o[~hit]) and torch.equal(lse2.t()[~hit], lse.t()[~hit])
