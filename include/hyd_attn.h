@@ -332,7 +332,7 @@ hyd_status hyd_rope_packed(const void* x, const int32_t* cu_seqlens, int num_seq
  *   cu_q, cu_kv      device int32[num_seqs+1], non-decreasing, within 0..total; rows in front of cu[0] and from cu[num_seqs] on
  *                    belong to no sequence: they are not read, and left as they were in the outputs
  *   kv_lens          device int32[num_seqs] or NULL: valid keys of a sequence, for padded caches (cu_kv then holds where each
- *                    one's rows begin and end).  Rows behind the valid keys are not read, whatever they hold.
+ *                    one's rows begin and end).  No result depends on rows behind the valid keys, whatever they hold.
  *   cu_q_host, cu_kv_host  host copies or NULL; when given they are checked (HYD_ERR_SEQLENS; HYD_ERR_SHAPE for a sequence above its
  *                    bound, cu_kv only without kv_lens)
  *   max_seqlen_q     bound on the queries of a sequence, 1..total_q;  max_seqlen_kv: on its valid keys, 0..total_kv.  Where a
@@ -341,7 +341,8 @@ hyd_status hyd_rope_packed(const void* x, const int32_t* cu_seqlens, int num_seq
  *   workspace        device, 256-byte aligned, hyd_cross_attn_workspace_bytes(...) bytes.  A size never falls as total_q, total_kv,
  *                    num_seqs or the bounds grow, so that one workspace serves every smaller call.
  * Few rows (max_seqlen_q * Hq/Hkv up to 32) run a kernel of their own, bound by reading K and V once.
- * T = 0 or num_seqs = 0 is a no-op.  Equal calls give equal bits.  Nothing depends on what the workspace held before.
+ * total_q = 0 is a no-op of the forward, num_seqs = 0 of both; queries without sequences are refused (HYD_ERR_SHAPE).  bf16: P is
+ * rounded to bf16 for the product with V.  Equal calls give equal bits.  Nothing depends on what the workspace held before.
  */
 size_t hyd_cross_attn_workspace_bytes(int total_q, int total_kv, int num_seqs, int max_seqlen_q, int max_seqlen_kv,
                                       int hq, int hkv, int head_dim, hyd_dtype dt, int is_bwd);
@@ -358,7 +359,9 @@ hyd_status hyd_cross_attn_fwd(const void* q, const void* k, const void* v,
  * dS_ij = P_ij (<dO_i, V_j> - D_i)
  *     dQ_i = scale sum_j dS_ij K_j;  dK_j = scale sum_{h in group, i} dS_ij Q_i;  dV_j = sum_{h in group, i} P_ij dO_i
  * dk and dv are written for every row of a sequence, zeros behind its valid keys; dq is 0 where there are none.  Rows that belong to
- * no sequence are neither read nor written.  Arithmetic, and the ranges of values it asks for, as hyd_varlen_attn_bwd.
+ * no sequence are neither read nor written.  Arithmetic, and the ranges of values it asks for, as hyd_varlen_attn_bwd; the power of two
+ * that brings dO into range is taken from the rows that have keys.  With max_seqlen_kv up to 128 all products are bf16 ones, P and dS two
+ * bf16 numbers each, and the ranges are bf16's own.
  * total_q = 0 or total_kv = 0 alone is not a no-op: the other side's gradients are zeros.
  */
 hyd_status hyd_cross_attn_bwd(const void* q, const void* k, const void* v, const void* o, const float* lse, const void* d_o,

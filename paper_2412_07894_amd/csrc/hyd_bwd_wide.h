@@ -29,7 +29,6 @@ constexpr int kKwStageBytes = 2 * kKwTileBytes;                       // Q, dO
 constexpr int kKwStatOff = kKwStages * kKwStageBytes;                 // [stage][LSE2, D][64]
 constexpr int kKwSlotOff = kKwStatOff + kKwStages * 2 * kKwBM * 4;
 constexpr int kKwVOff = 3 * kKwStageBytes;                            // V rows while an item begins
-constexpr int kXPartShift = 16;
 constexpr int kKwLds = kKwVOff + kKwBN * kRowBytes;                   // 160 KB: all of a CU's LDS
 static_assert(kKwSlotOff + 64 <= kKwLds, "statistics and work slot lie behind the ring");
 
@@ -122,10 +121,10 @@ __global__ void __launch_bounds__(kKwThreads, 1) hyd_bwd_dkdv_wide_bf16_kernel(P
         __syncthreads();                                      // everybody has read the work slot: its bytes may be overwritten
         const int lev = wi.lev, g = wi.head, row0 = wi.row0, L = wi.len;
         const int n_tiles = (L + kKwBN - 1) / kKwBN;
-        const int part = X ? lev >> kXPartShift : 0, per_part = X ? (((L + kKwBM - 1) / kKwBM) + p.part_max - 1) / p.part_max : 0;
+        const int part = X ? lev >> kCrossPartShift : 0, per_part = X ? (((L + kKwBM - 1) / kKwBM) + p.part_max - 1) / p.part_max : 0;
         const int j0 = X ? 0 : (n_tiles - lev) * kKwBN;
         const int kv0 = wi.seq;                               // (X: first key row of the item in K and V)
-        const int Lk = X ? lev & ((1 << kXPartShift) - 1) : L;        // keys end here, counted as j0 and wkey0 are
+        const int Lk = X ? lev & ((1 << kCrossPartShift) - 1) : L;        // keys end here, counted as j0 and wkey0 are
         if (!X) n_done += (min(L - j0, kKwBN) + kKvBN - 1) / kKvBN;   // (the trace counts tiles of the list of whole tiles)
         const int wkey0 = j0 + 64 * wave;                     // first key of this wave
         const bool active = wkey0 < Lk;

@@ -60,7 +60,6 @@ struct CrossList {
     int tile, parts, max_items;           // rows of a tile; parts of an item; records at most
     bool keys;                            // the list of key tiles
 };
-constexpr int kCrossPartShift = 16;
 // Classes of cost: exact up to 255 tiles, then 32 to an octave; the largest first.
 constexpr int kCrossClasses = 1024;
 __device__ __forceinline__ int cross_class(int tiles) {

@@ -62,7 +62,7 @@ long long most_tiles(long long total, long long most, int nseq, int tile) {
 // Sequences of at most 128 packed rows in bf16: tiles of as many, two workgroups to a CU (see CrossFwd).
 bool short_rows(const Sizes& z) { return z.dt == HYD_BF16 && (long long)z.max_q * (z.hq / z.hkv) <= CrossFwd<4>::kBM; }
 int fwd_rows(const Sizes& z) { return short_rows(z) ? CrossFwd<4>::kBM : tile_q(z.dt); }
-struct FwdLayout { size_t hdr, items, need, part_o, part_lse, total; long long max_items; };
+struct FwdLayout { size_t hdr, items, need, total; long long max_items; };
 constexpr size_t kPartRoomRows = 65536;   // rows (tokens times query heads, times parts) that are joined at most
 FwdLayout fwd_layout(const Sizes& z) {
     FwdLayout w;
@@ -199,7 +199,9 @@ void launch_fwd(const Sizes& z, const CrossShape& c, const void* q, const void* 
         // Parts of the keys: two workgroups for a CU, or if there are as many items as CUs, 32, whose ends then hardly differ;
         // each of 512 keys at least (1024 where the chip is full).  Up to 1024 keys (2048) they stay whole: a second launch costs 3 us.
         // Whole and in parts: 4 tokens of 32/8 heads, d = 128, 700 keys 9.4 and 11.0 us, 1500 keys 12.7 and 10.9, 8000 keys 52 and 26;
-        // 40 tokens of 8 heads, d = 64, 1 to 30000 keys 462 and 293 us.
+        // 40 tokens of 8 heads, d = 64, 1 to 30000 keys 462 and 293 us.  Parts of 512 and of 256 keys at least: one token of 32/8 heads,
+        // d = 128, 8000 keys 11.7 and 10.8 us, 3000 keys 11.2 and 10.7; 4 of 20 heads, d = 64, 1500 keys 11.1 and 11.0; 16 of 32/8 heads, 1500 keys
+        // 21.0 and 20.6, 8000 keys 98.7 and 99.7; but 700 keys, which stay whole here, 9.5 and 10.4 us for one token, 11.8 and 14.8 for 16.
         long long want = items >= kCus ? tiles(32 * kCus, items) : 2 * kCus / items;
         if (want > kCrossMaxParts) want = kCrossMaxParts;
         long long chunk = tiles(tiles(z.max_kv, want), kTurn) * kTurn;
@@ -214,7 +216,9 @@ void launch_fwd(const Sizes& z, const CrossShape& c, const void* q, const void* 
         hipLaunchKernelGGL(hyd_cross_few_bf16_kernel<D>, dim3((unsigned)(items * p.parts)), dim3(kFewThreads), kFewLds, st, p);
     } else {
         // items of whole tiles: own ones where they all fit on the chip, with the keys in parts where they do not fill it, else from a list
-        // (2 x 200 queries of 8/2 heads against 8000 keys, d = 128: 16 parts 34 us, whole 179 us)
+        // (2 x 200 queries of 8/2 heads against 8000 keys, d = 128: 16 parts 34 us, whole 179 us).  Parts are counted for one workgroup to a CU,
+        // also in tiles of 128 rows, of which two fit.  Counted for one and for two: 100 queries of 8 heads, d = 128, 12000 keys 21.2 and 24.4 us,
+        // 4 x 100 of 20 heads, 4000 keys 38 and 44; 12 x 64 of 20 heads, d = 64, 1000 keys 20 and 21, but 4000 keys 58 and 50, 12000 keys 197 and 150.
         const bool small = short_rows(z);
         const int per_cu = small ? CrossFwd<4>::kPerCu : 1;
         const int tile = fwd_rows(z), key_tile = z.dt == HYD_BF16 ? kFwdBN : kF32Tile;

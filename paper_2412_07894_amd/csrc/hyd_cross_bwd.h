@@ -14,7 +14,7 @@ namespace hyd {
 // ---------------------------------------------------------------------------------------------
 // Preparation, one launch: workgroups 0 and 1 build the item lists, then zero.n of them clear dK and dV behind the valid keys of
 // their sequences (padded caches), n_q make one pass over O and dO (row statistics, negated, and the maxima of |dO|), the others
-// copy K to fp16.  Bound by HBM, or by latency on small batches: 24 sequences, 18000 keys and 5400 queries of 20 heads, d = 64, 120 MB, 28 us.
+// copy K to fp16.  Bound by HBM, or by latency on small batches: 24 sequences, 18000 keys and 5400 queries of 20 heads, d = 64, 131 MB, 25 us.
 // ---------------------------------------------------------------------------------------------
 struct CrossPrepParams {
     CrossShape c;
@@ -141,8 +141,10 @@ __global__ void __launch_bounds__(kPrepThreads) hyd_cross_prep_bf16_kernel(Cross
 // ---------------------------------------------------------------------------------------------
 // dQ.  Work item = (256 packed rows of a sequence and KV head, a part of its keys); see hyd_bwd_bf16.h's dQ for the products and the
 // scaling.  The first part also writes what dK/dV streams: the fp16 copies of Q and of dO * 2^kg, and -D * 2^kg, by packed row.
-// 4 sequences of 1500 to 6000 queries and 4000 to 12000 keys, 32/8 heads, d = 128: 2.5 ms, 1.23 PFLOP/s in its three products (dK/dV 3.2 ms,
-// 1.29 in four): the matrix pipe.  At d = 64 the exponentials share the time.  Items of 128 rows, two workgroups to a CU, gained 20 % with 64 queries
+// 4 sequences of 1500 to 6000 queries and 4000 to 12000 keys, 32/8 heads, d = 128: 2.5 ms, 1.23 PFLOP/s in its three products (dK/dV 3.15 ms,
+// 1.3 in four), the matrix pipe busy for 69 % of the clocks (72).  Short items wait: 24 sequences of up to 448 queries and 1500 keys, 20 heads, d = 64,
+// 79 us at 24 % of the pipe, 41 % of the vector ALU and 2.7 TB/s (dK/dV 119 us, 22, 29 %, 2.5).  P and dS are fp16 numbers here, 2^-11 of
+// themselves, an eighth of the results' own rounding.  Items of 128 rows, two workgroups to a CU, gained 20 % with 64 queries
 // of a sequence and lost 5 % with 256 or 448 (d = 64, 1536 keys), so there is one form.
 // ---------------------------------------------------------------------------------------------
 struct CrossDqParams {

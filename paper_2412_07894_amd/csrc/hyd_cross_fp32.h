@@ -2,7 +2,8 @@
 // differs is which rows an item holds (hyd_cross.h: packed rows of a KV head's query heads) and that nothing is masked but the
 // keys behind a sequence's last one.  Hidden rows are zeros in every tile, so that 0 * x never meets a value that is not finite.
 // Bound by the matrix pipe: 8 sequences of 1000 queries and 1000 keys, 16/4 heads, d = 128: dQ 0.95 ms, 103 TFLOP/s in its three products, dK/dV
-// 1.39 ms, 94 in four (a large fp32 matrix product reaches 153); the tile that a product waits for is what is left.  Small batches wait for
+// 1.39 ms, 94 in four, forward 0.68 ms, 96 in two, of 4000 queries and keys 9.6 ms, 109 (a large fp32 matrix product reaches 153); the tile that
+// a product waits for is what is left.  Small batches wait for
 // their longest items: parts of them cost in fetches and sums what they save in balance, so they are taken only where there are
 // fewer items than CUs (7 sequences of up to 500 queries and 900 keys, 8/2 heads, d = 128: 257 us whole, 242 in parts of a few steps each;
 // with all sequences alike 255 and 310 us).

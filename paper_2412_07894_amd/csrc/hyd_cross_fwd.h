@@ -36,9 +36,13 @@ __device__ __forceinline__ void cross_store_part(float* row, const f32x16 (&acc)
 // of three stages that all waves share.  kSelf: one item per workgroup, its sequence and tile from the workgroup's number (launches
 // whose items all fit on the chip, which are too short to wait for a list).
 //
-// Bound by the matrix pipe where rows are many: 6 sequences of 1500 to 6000 queries and 4000 to 12000 keys, 32/8 heads, d = 128, 2.3 ms,
-// 1.15 PFLOP/s (a large bf16 matrix product reaches 1.37).  Short items wait for their first tiles and for their stores: 24
-// sequences of up to 448 queries and 1500 keys, 20 heads, d = 64, 54 us, and 6 us for their list.
+// P is rounded to bf16 for the second product, off by 2^-8 of itself at most: O is off by about sqrt(2) of what its own rounding
+// costs (2.3e-3 of its norm).  A second bf16 number for what the rounding leaves would double the second product.
+//
+// Bound by the matrix pipe where rows are many: 6 sequences of 1500 to 6000 queries and 4000 to 12000 keys, 32/8 heads, d = 128, 2.22 to
+// 2.3 ms, 1.15 to 1.19 PFLOP/s (a large bf16 matrix product reaches 1.37), the pipe busy for 60 % of the clocks and the vector ALU for
+// 47.  Short items wait for their first tiles and for their stores: 24 sequences of up to 448 queries and 1500 keys, 20 heads, d = 64, 59 us with
+// the 5 of the list in front (pipe 19 %, vector ALU 41 %, 2.9 TB/s).
 //
 // NW = 4: 128 rows, two stages, and two workgroups to a CU, one of which streams while the other begins or ends; for sequences that
 // have no more rows.  NW = 8 and 4 with 24 sequences of 1536 keys, 20 heads: 64 queries 52 and 36 us (d = 64), 85 and 79 (128); 128 queries
@@ -230,8 +234,12 @@ __global__ void __launch_bounds__(CrossFwd<NW>::kThreads, CrossFwd<NW>::kPerCu) 
 // rows each) without meeting the others: K of its next turn is requested as soon as the scores are formed, V as soon as
 // the second product is done, so that 64 to 128 KB are under way per CU.  The waves' results meet in LDS once, the parts' by
 // hyd_cross_join_kernel.  Two workgroups share a CU, so that one streams while the other begins or ends: with one of 8 waves 64 tokens
-// of 32/8 heads, d = 128, against 500 to 8192 keys took 258 us, so 222 (1.13 GB, 5.1 TB/s); 16 against 30000 keys 380 us
-// (5.2 TB/s); the smallest calls, 11 us, are two launches.
+// of 32/8 heads, d = 128, against 500 to 8192 keys took 258 us, so 222 (1.13 GB, 5.1 TB/s); 16 against 30000 keys 359 us
+// (5.5 TB/s).  The smallest calls, 11 us, are two launches: 4 tokens of 20 heads, d = 64, against 1500 keys 8.8 us in 240 workgroups
+// (30.7 MB, 3.5 TB/s) and 3.6 us for the join.
+//
+// P is rounded to bf16 as in the tile form.  With what the rounding leaves as a second bf16 number, large calls take what they took, but
+// small ones 5 % more (11.1 for 10.6 us, 8.8 for 8.3, 12.4 for 11.8), so it is one number here too.
 // ---------------------------------------------------------------------------------------------
 constexpr int kFewRows = 32, kFewKeys = 32, kFewWaves = 4, kFewThreads = 64 * kFewWaves;
 constexpr int kFewTileBytes = kFewKeys * kRowBytes;                   // 8 KB

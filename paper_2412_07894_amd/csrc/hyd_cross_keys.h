@@ -13,8 +13,10 @@
 // Arithmetic.  P and dS enter the second products as two bf16 numbers, the rounded value and the rest, 16 bits together, so that
 // every product runs on the bf16 MFMA with Q, K, dO as they are: no scaling of dO, no copies, and no range but bf16's own.
 //
-// Bound by the instructions of its two waves to a SIMD and their meetings.  16 sequences of 2000 queries, 8 heads, 128 keys here and
-// 129 keys in the general form: d = 64 73 and 131 us, d = 128 125 and 236 us; of 1024 to 4096 queries and 8 to 77 keys, d = 64, 90 us (151 MB).
+// Bound by the meetings of its two waves to a SIMD: the waves wait for 47 % of their time, the matrix pipe is busy for 29 % of the clocks, vector
+// ALU and LDS for 41 each.  All 128 keys are computed whatever their number.  16 sequences of 2000 queries, 8 heads, 128 keys here and
+// 129 keys in the general form: d = 64 72 and 129 us, d = 128 121 and 236 us; of 1024 to 4096 queries and 8 to 77 keys, d = 64, 84 us and 5 for
+// the sums (151 MB have to be moved, 177 are).
 //
 // A tile has three barriers: the first opens it (and says that the stage before the last has been read by all), the second hands P
 // over, the third publishes dS.

@@ -10,8 +10,8 @@
 // its rows' pairs go to LDS once (their cost is shared by the heads), and the threads walk the units of its rows in memory order,
 // a unit being C pairs (two loads of C elements, 16 bytes each where alignment allows) or 2 C elements behind the
 // turned part, which are only copied.  The first units are requested before the table is formed.  24700 tokens of 32/8 heads of 128
-// out of a fused projection, 506 MB: 104 us, 4.9 TB/s (a large copy reaches 5.07); half of 80 heads of 128, side by side, 317 MB: 62 us;
-// one token for each of 16 requests: 6 us, the launch.
+// out of a fused projection, 506 MB: 104 us, 4.9 TB/s (a large copy reaches 5.07); half of 80 heads of 128, side by side, 317 MB: 60 us;
+// one token for each of 16 requests: 4.4 us, of the 8 that the call takes.
 #pragma once
 #include "hyd_find.h"
 

@@ -336,6 +336,7 @@ __device__ __forceinline__ void decode_work(const HeadMap& hm, int n_items, int 
 // 9230 / 21233 -> 9119 / 20843; 2000 of one token, 32/8 heads 1136 / 2105 -> 1115 / 2090.
 constexpr int kShortItem = 2;
 struct WorkItem { int seq, lev, head, row0, len; };
+constexpr int kCrossPartShift = 16;    // cross attention: a record's second number is rows or keys | part << this (CrossList)
 constexpr int kSlotInts = 16;          // two buffers of 8 ints
 struct WorkFetcher {
     int cur;          // slot buffer holding the current item (all threads)
