@@ -360,8 +360,8 @@ hyd_status hyd_cross_attn_fwd(const void* q, const void* k, const void* v,
  *     dQ_i = scale sum_j dS_ij K_j;  dK_j = scale sum_{h in group, i} dS_ij Q_i;  dV_j = sum_{h in group, i} P_ij dO_i
  * dk and dv are written for every row of a sequence, zeros behind its valid keys; dq is 0 where there are none.  Rows that belong to
  * no sequence are neither read nor written.  Arithmetic, and the ranges of values it asks for, as hyd_varlen_attn_bwd; the power of two
- * that brings dO into range is taken from the rows that have keys.  With max_seqlen_kv up to 128 all products are bf16 ones, P and dS two
- * bf16 numbers each, and the ranges are bf16's own.
+ * that brings dO into range is taken from the rows that have keys.  In bf16 with max_seqlen_kv up to 128 all products are bf16 ones, P and
+ * dS two bf16 numbers each, and the ranges are bf16's own (not from num_seqs * Hkv = 2^23 on).
  * total_q = 0 or total_kv = 0 alone is not a no-op: the other side's gradients are zeros.
  */
 hyd_status hyd_cross_attn_bwd(const void* q, const void* k, const void* v, const void* o, const float* lse, const void* d_o,
